@@ -64,6 +64,8 @@ enum { MOE_MODE_FUSED = 0, MOE_MODE_GEMM_ONLY = 1, MOE_MODE_COMBINE_ONLY = 2 };
  * tiles has them; the launch reads k_tot) and to its real width min(T_N^comm, ceil(H/L)). */
 enum { MOE_RHO_PAPER = 0, MOE_RHO_LOCAL = 1 };
 enum { MOE_DEP_SPLIT = 0, MOE_DEP_TILE = 1 };
+/* element types of the operators that take more than bf16 */
+enum { MOE_BF16 = 0, MOE_FP16 = 1, MOE_FP32 = 2 };
 #define MOE_MAX_EP 8
 #define MOE_MAX_L 8
 #define MOE_MTILES_ON_DEVICE (-1)   /* moe_gemm2_combine: read the m-tile count from routing->tiles[E_tot] on the device */
@@ -448,6 +450,81 @@ int32_t moe_layer_host(moe_handle *h, const void *x_routed_host, const int32_t *
                        int32_t tile_m, int32_t tile_n, const moe_sm_limits *limits_or_null,
                        void *arena, size_t arena_bytes, int32_t *tile_counts_pinned,
                        void *out_host, moe_plan *plan_out, void *stream);
+
+/* ==== the steps of the layer as operators of their own ====================================================
+ * Matrices are row-major with a distance `ld` between rows, in elements: ld >= columns, a multiple of 8, the matrix 16-byte
+ * aligned.  dtype: MOE_BF16, MOE_FP16 or MOE_FP32, of every floating-point matrix of a call.  Sums and activations are computed in
+ * fp32 and rounded once.  Nothing is allocated and no workspace is used, a call is one launch and can be captured into a graph,
+ * inputs and outputs do not overlap unless said otherwise, no result depends on the order of atomics.  Every call returns
+ * MOE_ERR_NULL, MOE_ERR_SHAPE, MOE_ERR_ALIGN or MOE_ERR_UNSUPPORTED for arguments it does not take, and MOE_OK without a launch where
+ * there are no rows.  An index that is out of range is reported in the status word (MOE_DEV_OOB), and what it names is skipped.
+ *
+ * ---- tokens to expert rows and back (Section II-A), with their gradients ---------------------------------
+ * inv_perm [device] int32 [T, k_tot]: the row of every assignment, as moe_build_routing leaves it in routing.inv_perm; -1: the
+ * assignment has no row and counts nothing; no row is named twice.  Of the shape T, H and k_tot are used (H % 8 == 0,
+ * k_tot <= 32); tokens are [T, H], rows [T * k_tot, H], topk_w [device] fp32 [T, k_tot].
+ *   moe_permute         rows[inv_perm[t][j]] = tokens[t]                 (rows that no assignment names stay as they are)
+ *   moe_permute_grad    d_tokens[t] = sum_j d_rows[inv_perm[t][j]]
+ *   moe_unpermute       out[t] = sum_j topk_w[t][j] * rows[inv_perm[t][j]]
+ *   moe_unpermute_grad  d_rows[inv_perm[t][j]] = topk_w[t][j] * d_out[t]; d_topk_w[t][j] = <d_out[t], rows[inv_perm[t][j]]>
+ *                       (0 without a row); d_rows may be rows itself, with the same ld
+ * A weight times an infinity or no number follows IEEE arithmetic; the rows of other tokens are not touched by it. */
+int32_t moe_permute(moe_handle *h, const void *tokens, int64_t ld_tokens, const int32_t *inv_perm, const moe_shape *shape,
+                    int32_t dtype, void *rows, int64_t ld_rows, uint32_t *status_dev, void *stream);
+int32_t moe_permute_grad(moe_handle *h, const void *d_rows, int64_t ld_rows, const int32_t *inv_perm, const moe_shape *shape,
+                         int32_t dtype, void *d_tokens, int64_t ld_tokens, uint32_t *status_dev, void *stream);
+int32_t moe_unpermute(moe_handle *h, const void *rows, int64_t ld_rows, const int32_t *inv_perm, const float *topk_w,
+                      const moe_shape *shape, int32_t dtype, void *out, int64_t ld_out, uint32_t *status_dev, void *stream);
+int32_t moe_unpermute_grad(moe_handle *h, const void *d_out, int64_t ld_out, const void *rows, int64_t ld_rows,
+                           const int32_t *inv_perm, const float *topk_w, const moe_shape *shape, int32_t dtype, void *d_rows,
+                           int64_t ld_d_rows, float *d_topk_w, uint32_t *status_dev, void *stream);
+
+/* ---- gated activation, its 8-bit checkpoint and its backward pass ------------------------------------------
+ * gate_up [rows, 2 I]: gate in the first I columns, up behind it (the products with W1 [2, I, H] of an expert); act [rows, I] =
+ * silu(gate) * up.  I % 16 == 0.  codes and scales, both or neither (NULL: nothing is kept): gate and up in 8 bits for the
+ * backward pass,
+ *   codes  [device] uint8 [rows, 2 I], 16-byte aligned: e4m3;
+ *   scales [device] uint8 [rows, 2, ceil(I / 32)]: for 32 columns of gate (of up) the exponent, biased by 127, of the power of two
+ *          that their codes are multiplied by, the smallest at which none of them exceeds 448.
+ * A value that is infinite or no number is kept as no number; the others of its 32 are not affected.
+ * moe_gated_act_grad reads the checkpoint alone: d_gate_up [rows, 2 I] from d_act [rows, I], with g, u the values kept,
+ *   d_gate = d_act u s (1 + g (1 - s)), d_up = d_act g s, s = 1 / (1 + exp(-g));
+ * act_or_null [rows, I] (ld_act): silu(g) * u of the values kept, which the gradient of the next weights needs; NULL: not wanted. */
+int32_t moe_gated_act(moe_handle *h, const void *gate_up, int64_t ld_gate_up, int32_t rows, int32_t I, int32_t dtype, void *act,
+                      int64_t ld_act, void *codes_or_null, void *scales_or_null, void *stream);
+int32_t moe_gated_act_grad(moe_handle *h, const void *d_act, int64_t ld_d_act, const void *codes, const void *scales, int32_t rows,
+                           int32_t I, int32_t dtype, void *d_gate_up, int64_t ld_d_gate_up, void *act_or_null, int64_t ld_act,
+                           void *stream);
+
+/* ---- microscaled 4-bit floating point: quantisation and grouped product ------------------------------------
+ * 32 consecutive columns share a power of two, floor(log2(amax)) - 2 clamped to [-127, 127]; values divided by it are rounded to
+ * e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign), to the nearest, ties to even, saturating at 6.  32 columns with an infinity or no number
+ * are no number, all of them.  K % 32 == 0.
+ *   codes  [device] uint8 [rows, K / 2], 16-byte aligned: the even column in the low four bits;
+ *   scales [device] moe_mxfp4_scale_bytes(rows, K, groups) bytes, 16-byte aligned: exponents biased by 127 (255: no number), laid out as
+ *          the tensor cores take them: blocks of 128 rows x 128 columns, the blocks of 128 rows side by side (ceil(K / 128) of
+ *          them), 512 bytes each, row i and columns 32 s .. 32 s + 31 of a block at byte 16 (i % 32) + 4 (i / 32) + s.  Rows come in groups
+ *          (experts): row r of group g, whose rows begin at o, is row (r - o) % 128 of row block o / 128 + g + (r - o) / 128.
+ *          Exponents of columns past K are written as 0 and have to be less than 255 in a buffer that another program fills.
+ * Groups: offsets_or_null [device] int32 [groups + 1], from 0 up (routing.offsets; rows from the last entry on stay as
+ * they are), or NULL: rows / groups rows each (weights [E, N, K] are rows E * N in E groups).
+ * moe_mxfp4_quantize: src [rows, K].  With inv_perm_or_null [device] int32 [rows / copies, copies], src is [rows / copies, K] and row t is put
+ * into rows inv_perm[t][0 ..] (-1: none): tokens are quantised once, into routed order.  Without it copies = 1.
+ * moe_mxfp4_dequantize: out [rows, K] = codes times their powers of two. */
+int32_t moe_mxfp4_scale_bytes(int32_t rows, int32_t K, int32_t groups, size_t *bytes);
+int32_t moe_mxfp4_quantize(moe_handle *h, const void *src, int64_t ld_src, int32_t dtype, int32_t rows, int32_t K, int32_t groups,
+                           const int32_t *offsets_or_null, const int32_t *inv_perm_or_null, int32_t copies, void *codes,
+                           void *scales, uint32_t *status_dev, void *stream);
+int32_t moe_mxfp4_dequantize(moe_handle *h, const void *codes, const void *scales, int32_t rows, int32_t K, int32_t groups,
+                             const int32_t *offsets_or_null, int32_t dtype, void *out, int64_t ld_out, uint32_t *status_dev,
+                             void *stream);
+/* out[r][n] = sum_k x[r][k] * w[e][n][k] for the rows r of expert e (offsets[e] <= r < offsets[e + 1]), one persistent tcgen05 launch.
+ * x_codes [rows, K / 2] with x_scales in E_tot groups by `offsets` [device] int32 [E_tot + 1]; w_codes [E_tot, N, K / 2] with w_scales in E_tot
+ * groups of N rows.  N % 8 == 0, E_tot <= 1024.  dtype of out [rows, N]: MOE_BF16 or MOE_FP16.  fp32 accumulation.  Rows from
+ * offsets[E_tot] on stay as they are.  Offsets that go back or past `rows` are reported and the rows they name skipped. */
+int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void *x_scales, const void *w_codes, const void *w_scales,
+                       const int32_t *offsets, int32_t rows, int32_t E_tot, int32_t N, int32_t K, int32_t dtype, void *out,
+                       int64_t ld_out, uint32_t *status_dev, void *stream);
 
 #ifdef __cplusplus
 }

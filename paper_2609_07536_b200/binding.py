@@ -24,6 +24,7 @@ MOE_DEV_OK, MOE_DEV_TIMEOUT, MOE_DEV_OOB, MOE_DEV_DUP_EXPERT = 0, 1, 2, 3
 MOE_MODE_FUSED, MOE_MODE_GEMM_ONLY, MOE_MODE_COMBINE_ONLY = 0, 1, 2
 MOE_RHO_PAPER, MOE_RHO_LOCAL = 0, 1
 MOE_DEP_SPLIT, MOE_DEP_TILE = 0, 1
+MOE_BF16, MOE_FP16, MOE_FP32 = 0, 1, 2
 MOE_MAX_EP, MOE_MAX_L = 8, 8
 MOE_MTILES_ON_DEVICE = -1
 
@@ -36,6 +37,8 @@ EXPORTS = [
     "moe_layer", "moe_calibrate_rho", "moe_host_arena_bytes", "moe_layer_host",
     "moe_gemm1_workspace_bytes", "moe_gemm1_act", "moe_post_router_layer", "moe_set_timeline",
     "moe_select_tile", "moe_release_workspace", "moe_set_probe",
+    "moe_permute", "moe_permute_grad", "moe_unpermute", "moe_unpermute_grad", "moe_gated_act", "moe_gated_act_grad",
+    "moe_mxfp4_scale_bytes", "moe_mxfp4_quantize", "moe_mxfp4_dequantize", "moe_mxfp4_gemm",
 ]
 
 
@@ -145,6 +148,17 @@ def lib():
         L.moe_host_arena_bytes.argtypes = [P(moe_shape), i32, i32, P(C.c_size_t)]
         L.moe_layer_host.argtypes = [vp, vp, vp, vp, vp, P(moe_shape), i32, i32, P(moe_sm_limits), vp,
                                      C.c_size_t, vp, vp, P(moe_plan), vp]
+        i64 = C.c_int64
+        L.moe_permute.argtypes = [vp, vp, i64, vp, P(moe_shape), i32, vp, i64, vp, vp]
+        L.moe_permute_grad.argtypes = [vp, vp, i64, vp, P(moe_shape), i32, vp, i64, vp, vp]
+        L.moe_unpermute.argtypes = [vp, vp, i64, vp, vp, P(moe_shape), i32, vp, i64, vp, vp]
+        L.moe_unpermute_grad.argtypes = [vp, vp, i64, vp, i64, vp, vp, P(moe_shape), i32, vp, i64, vp, vp, vp]
+        L.moe_gated_act.argtypes = [vp, vp, i64, i32, i32, i32, vp, i64, vp, vp, vp]
+        L.moe_gated_act_grad.argtypes = [vp, vp, i64, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp]
+        L.moe_mxfp4_scale_bytes.argtypes = [i32, i32, i32, P(C.c_size_t)]
+        L.moe_mxfp4_quantize.argtypes = [vp, vp, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp]
+        L.moe_mxfp4_dequantize.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, i64, vp, vp]
+        L.moe_mxfp4_gemm.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp, vp]
         for name in EXPORTS:
             if name != "moe_last_cuda_error":
                 getattr(L, name).restype = i32
@@ -402,6 +416,172 @@ def moe_layer_host(h, x_routed_host, topk_idx_host, topk_w_host, W2_dev, shape, 
                                 _ptr(tile_counts_pinned), _ptr(out_host), C.byref(plan), _stream(stream)),
            "moe_layer_host", h)
     return plan
+
+
+# ----------------------------------------------------------------------------- the layer's steps as operators of their own
+#
+# These take their sizes, element type and row distance from the tensors, and refuse tensors that do not fit together with the
+# status code that the library has for it.
+
+_types = {}
+
+
+def _row_type(t, who):
+    if not _types:
+        import torch
+        _types.update({torch.bfloat16: MOE_BF16, torch.float16: MOE_FP16, torch.float32: MOE_FP32})
+    code = _types.get(t.dtype)
+    if code is None:
+        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"element type {t.dtype}")
+    return code
+
+
+def _on_device(h_device, t, who, what):
+    if t.get_device() != h_device:
+        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is on {t.device}, the current CUDA device is {h_device}")
+
+
+def _matrix(t, rows, cols, like, device, who, what):
+    """(address, row distance) of a matrix of at least `rows` x exactly `cols` with contiguous columns."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] < rows or shape[1] != cols:
+        raise MoeError(MOE_ERR_SHAPE, who, f"{what} is {tuple(shape)}, not [{rows}, {cols}]")
+    if t.dtype != like:
+        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is {t.dtype}, not {like}")
+    _on_device(device, t, who, what)
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise MoeError(MOE_ERR_SHAPE, who, f"the columns of {what} are not contiguous")
+    return t.data_ptr(), ld if shape[0] > 1 else max(ld, cols) if ld % 8 == 0 else cols
+
+
+def _vector(t, n, kind, device, who, what):
+    """Address of `n` contiguous elements of torch type `kind` (a raw address, or None, is passed on)."""
+    if t is None or isinstance(t, int):
+        return t
+    if str(t.dtype) != kind:
+        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is {t.dtype}, not {kind}")
+    if t.numel() < n or not t.is_contiguous():
+        raise MoeError(MOE_ERR_SHAPE, who, f"{what} is not {n} contiguous elements")
+    _on_device(device, t, who, what)
+    return t.data_ptr()
+
+
+def _device():
+    import torch
+    return torch.cuda.current_device()
+
+
+def moe_permute(h, tokens, inv_perm, shape, rows, status_dev, stream=None):
+    """rows[inv_perm[t][j]] = tokens[t]; inv_perm: int32 [T, k_tot] tensor, or routing.inv_perm."""
+    who, dev, R = "moe_permute", _device(), shape.T * shape.k_tot
+    a, lda = _matrix(tokens, shape.T, shape.H, tokens.dtype, dev, who, "tokens")
+    b, ldb = _matrix(rows, R, shape.H, tokens.dtype, dev, who, "rows")
+    _check(lib().moe_permute(h, a, lda, _vector(inv_perm, R, "torch.int32", dev, who, "inv_perm"), C.byref(shape), _row_type(tokens, who), b, ldb,
+                             _ptr(status_dev), _stream(stream)), who, h)
+
+
+def moe_permute_grad(h, d_rows, inv_perm, shape, d_tokens, status_dev, stream=None):
+    """d_tokens[t] = sum over j of d_rows[inv_perm[t][j]]."""
+    who, dev, R = "moe_permute_grad", _device(), shape.T * shape.k_tot
+    a, lda = _matrix(d_rows, R, shape.H, d_rows.dtype, dev, who, "d_rows")
+    b, ldb = _matrix(d_tokens, shape.T, shape.H, d_rows.dtype, dev, who, "d_tokens")
+    _check(lib().moe_permute_grad(h, a, lda, _vector(inv_perm, R, "torch.int32", dev, who, "inv_perm"), C.byref(shape), _row_type(d_rows, who), b, ldb,
+                                  _ptr(status_dev), _stream(stream)), who, h)
+
+
+def moe_unpermute(h, rows, inv_perm, topk_w, shape, out, status_dev, stream=None):
+    """out[t] = sum over j of topk_w[t][j] * rows[inv_perm[t][j]]."""
+    who, dev, R = "moe_unpermute", _device(), shape.T * shape.k_tot
+    a, lda = _matrix(rows, R, shape.H, rows.dtype, dev, who, "rows")
+    b, ldb = _matrix(out, shape.T, shape.H, rows.dtype, dev, who, "out")
+    _check(lib().moe_unpermute(h, a, lda, _vector(inv_perm, R, "torch.int32", dev, who, "inv_perm"),
+                               _vector(topk_w, R, "torch.float32", dev, who, "topk_w"), C.byref(shape), _row_type(rows, who), b, ldb,
+                               _ptr(status_dev), _stream(stream)), who, h)
+
+
+def moe_unpermute_grad(h, d_out, rows, inv_perm, topk_w, shape, d_rows, d_topk_w, status_dev, stream=None):
+    """d_rows[inv_perm[t][j]] = topk_w[t][j] * d_out[t]; d_topk_w[t][j] = <d_out[t], rows[inv_perm[t][j]]>."""
+    who, dev, R = "moe_unpermute_grad", _device(), shape.T * shape.k_tot
+    a, lda = _matrix(d_out, shape.T, shape.H, d_out.dtype, dev, who, "d_out")
+    b, ldb = _matrix(rows, R, shape.H, d_out.dtype, dev, who, "rows")
+    c, ldc = _matrix(d_rows, R, shape.H, d_out.dtype, dev, who, "d_rows")
+    _check(lib().moe_unpermute_grad(h, a, lda, b, ldb, _vector(inv_perm, R, "torch.int32", dev, who, "inv_perm"),
+                                    _vector(topk_w, R, "torch.float32", dev, who, "topk_w"), C.byref(shape), _row_type(d_out, who), c, ldc,
+                                    _vector(d_topk_w, R, "torch.float32", dev, who, "d_topk_w"), _ptr(status_dev), _stream(stream)), who, h)
+
+
+def moe_gated_act(h, gate_up, act, codes=None, scales=None, stream=None):
+    """act [rows, I] = silu(gate) * up of gate_up [rows, 2 I]; codes uint8 [rows, 2 I] and scales uint8 [rows, 2 ceil(I / 32)]: the
+    8-bit copy for the backward pass."""
+    who, dev = "moe_gated_act", _device()
+    rows, I = gate_up.shape[0], gate_up.shape[-1] // 2
+    a, lda = _matrix(gate_up, rows, 2 * I, gate_up.dtype, dev, who, "gate_up")
+    b, ldb = _matrix(act, rows, I, gate_up.dtype, dev, who, "act")
+    _check(lib().moe_gated_act(h, a, lda, rows, I, _row_type(gate_up, who), b, ldb, _vector(codes, rows * 2 * I, "torch.uint8", dev, who, "codes"),
+                               _vector(scales, rows * 2 * ((I + 31) // 32), "torch.uint8", dev, who, "scales"), _stream(stream)), who, h)
+
+
+def moe_gated_act_grad(h, d_act, codes, scales, d_gate_up, act=None, stream=None):
+    """d_gate_up [rows, 2 I] from d_act [rows, I] and the 8-bit copy; act [rows, I]: the activation of the values kept, again."""
+    who, dev = "moe_gated_act_grad", _device()
+    rows, I = d_act.shape[0], d_act.shape[-1]
+    a, lda = _matrix(d_act, rows, I, d_act.dtype, dev, who, "d_act")
+    b, ldb = _matrix(d_gate_up, rows, 2 * I, d_act.dtype, dev, who, "d_gate_up")
+    c, ldc = _matrix(act, rows, I, d_act.dtype, dev, who, "act") if act is not None else (None, 0)
+    _check(lib().moe_gated_act_grad(h, a, lda, _vector(codes, rows * 2 * I, "torch.uint8", dev, who, "codes"),
+                                    _vector(scales, rows * 2 * ((I + 31) // 32), "torch.uint8", dev, who, "scales"), rows, I, _row_type(d_act, who),
+                                    b, ldb, c, ldc, _stream(stream)), who, h)
+
+
+def moe_mxfp4_scale_bytes(rows: int, K: int, groups: int) -> int:
+    b = C.c_size_t()
+    _check(lib().moe_mxfp4_scale_bytes(rows, K, groups, C.byref(b)), "moe_mxfp4_scale_bytes")
+    return b.value
+
+
+def _mxfp4_operand(codes, scales, groups, dev, who, what=""):
+    """(address of the codes, address of the exponents, rows, K); codes uint8 [..., K / 2] contiguous."""
+    rows, K = codes.numel() // max(1, codes.shape[-1]), 2 * codes.shape[-1]
+    need = moe_mxfp4_scale_bytes(rows, K, groups)
+    return (_vector(codes, rows * K // 2, "torch.uint8", dev, who, what + "codes"), _vector(scales, need, "torch.uint8", dev, who, what + "scales"), rows, K)
+
+
+def moe_mxfp4_quantize(h, src, codes, scales, groups, status_dev, offsets=None, inv_perm=None, stream=None):
+    """src [rows, K] -> codes uint8 [rows, K / 2] and scales (moe_mxfp4_scale_bytes) in `groups` groups: by offsets int32
+    [groups + 1], or of equally many rows.  inv_perm int32 [T, copies]: src is [T, K], row t goes to the rows inv_perm[t]."""
+    who, dev = "moe_mxfp4_quantize", _device()
+    c, sc, rows, K = _mxfp4_operand(codes, scales, groups, dev, who)
+    copies = 1 if inv_perm is None else inv_perm.shape[-1]
+    if inv_perm is not None and inv_perm.numel() != rows:
+        raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm names {inv_perm.numel()} rows, codes have {rows}")
+    a, lda = _matrix(src, rows // max(1, copies), K, src.dtype, dev, who, "src")
+    _check(lib().moe_mxfp4_quantize(h, a, lda, _row_type(src, who), rows, K, groups, _vector(offsets, groups + 1, "torch.int32", dev, who, "offsets"),
+                                    _vector(inv_perm, rows, "torch.int32", dev, who, "inv_perm"), copies, c, sc, _ptr(status_dev), _stream(stream)), who, h)
+
+
+def moe_mxfp4_dequantize(h, codes, scales, groups, out, status_dev, offsets=None, stream=None):
+    """out [rows, K] = the values that codes and scales stand for."""
+    who, dev = "moe_mxfp4_dequantize", _device()
+    c, sc, rows, K = _mxfp4_operand(codes, scales, groups, dev, who)
+    a, lda = _matrix(out, rows, K, out.dtype, dev, who, "out")
+    _check(lib().moe_mxfp4_dequantize(h, c, sc, rows, K, groups, _vector(offsets, groups + 1, "torch.int32", dev, who, "offsets"), _row_type(out, who),
+                                      a, lda, _ptr(status_dev), _stream(stream)), who, h)
+
+
+def moe_mxfp4_gemm(h, x_codes, x_scales, w_codes, w_scales, offsets, out, status_dev, stream=None):
+    """out[r] = w[e] x[r] for the rows r of expert e, offsets[e] <= r < offsets[e + 1]; w_codes uint8 [E_tot, N, K / 2]."""
+    who, dev = "moe_mxfp4_gemm", _device()
+    if len(w_codes.shape) != 3 or len(x_codes.shape) != 2:
+        raise MoeError(MOE_ERR_SHAPE, who, "w_codes is [E_tot, N, K / 2], x_codes [rows, K / 2]")
+    E, N = w_codes.shape[0], w_codes.shape[1]
+    w, ws, w_rows, Kw = _mxfp4_operand(w_codes, w_scales, E, dev, who, "w_")
+    x, xs, rows, K = _mxfp4_operand(x_codes, x_scales, E, dev, who, "x_")
+    if K != Kw:
+        raise MoeError(MOE_ERR_SHAPE, who, f"x has {K} columns, w {Kw}")
+    a, lda = _matrix(out, rows, N, out.dtype, dev, who, "out")
+    _check(lib().moe_mxfp4_gemm(h, x, xs, w, ws, _vector(offsets, E + 1, "torch.int32", dev, who, "offsets"), rows, E, N, K, _row_type(out, who), a, lda,
+                                _ptr(status_dev), _stream(stream)), who, h)
 
 
 # ----------------------------------------------------------------------------- device memory plumbing

@@ -41,6 +41,22 @@ Divisor divisor_of(int32_t d)
     return r;
 }
 
+// 128B swizzle, every element of a box; false, with a message in the handle, when it cannot be encoded
+static bool encode_map(moe_handle *h, CUtensorMap *map, CUtensorMapDataType type, const void *ptr, int rank, const cuuint64_t *dims,
+                       const cuuint64_t *strides, const cuuint32_t *box, const char *name)
+{
+    typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                      const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    const cuuint32_t es[5] = {1, 1, 1, 1, 1};
+    const CUresult cr = reinterpret_cast<EncodeTiledFn>(h->encode_tiled)(
+        map, type, (cuuint32_t)rank, const_cast<void *>(ptr), dims, strides, box, es,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (cr == CUDA_SUCCESS) return true;
+    snprintf(h->err, sizeof h->err, "cuTensorMapEncodeTiled(%s) failed: %d", name, (int)cr);
+    return false;
+}
+
 // The table's entry for these arguments, encoded if it is another one's.
 static const CUtensorMap *cached_map(moe_handle *h, const void *ptr, int32_t planes, int64_t rows, int32_t cols, int32_t box_rows, int rank,
                                      const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box, const char *name)
@@ -48,18 +64,8 @@ static const CUtensorMap *cached_map(moe_handle *h, const void *ptr, int32_t pla
     if (!h->maps && !(h->maps = new (std::nothrow) MapEntry[kMapEntries]())) return nullptr;
     MapEntry &m = h->maps[map_place(ptr, box_rows)];
     if (m.ptr == ptr && m.rows == rows && m.cols == cols && m.planes == planes && m.box_rows == box_rows) return &m.map;
-    typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                      const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    const cuuint32_t es[5] = {1, 1, 1, 1, 1};
     m.ptr = nullptr;
-    const CUresult cr = reinterpret_cast<EncodeTiledFn>(h->encode_tiled)(
-        &m.map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(ptr), dims, strides, box, es,
-        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (cr != CUDA_SUCCESS) {
-        snprintf(h->err, sizeof h->err, "cuTensorMapEncodeTiled(%s) failed: %d", name, (int)cr);
-        return nullptr;
-    }
+    if (!encode_map(h, &m.map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ptr, rank, dims, strides, box, name)) return nullptr;
     m.rows = rows;
     m.cols = cols;
     m.planes = planes;
@@ -74,6 +80,14 @@ const CUtensorMap *operand_map(moe_handle *h, const void *ptr, int32_t planes, i
     const cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * 2 * (cuuint64_t)rows};
     const cuuint32_t box[3] = {(cuuint32_t)kBlockK, (cuuint32_t)box_rows, 1};
     return cached_map(h, ptr, planes, rows, cols, box_rows, planes ? 3 : 2, dims, strides, box, name);
+}
+
+bool code_map(moe_handle *h, CUtensorMap *map, const void *ptr, int32_t planes, int64_t rows, int32_t row_bytes, int32_t box_rows, const char *name)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)row_bytes, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)row_bytes * (cuuint64_t)rows};
+    const cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1};
+    return encode_map(h, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, ptr, planes ? 3 : 2, dims, strides, box, name);
 }
 
 const CUtensorMap *gate_up_map(moe_handle *h, const void *ptr, int32_t experts, int32_t inter, int32_t cols, int32_t box_inter, const char *name)
@@ -159,6 +173,7 @@ int32_t moe_create(int32_t device, moe_handle **out)
     }
     e = routing_prepare(&h->routing_max_cluster);
     if (e == cudaSuccess) e = gemm1_prepare();
+    if (e == cudaSuccess) e = mxfp4_prepare();
     if (e != cudaSuccess) {
         delete h;
         return MOE_ERR_CUDA;

@@ -1,0 +1,218 @@
+// Gated activation between the two expert products (Section II-A), act = silu(gate) * up, on rows [gate | up], with gate and up kept in
+// 8 bits for the backward pass, and that backward pass, which reads nothing but the 8-bit copy:
+//   s = 1 / (1 + exp(-g)),  silu = g s,  d_up = d_act silu,  d_gate = d_act u s (1 + g (1 - s)),  act = silu u.
+// The copy: e4m3 codes, and for every 32 columns of gate and of up one byte e, the power of two 2^(e - 127) that the codes are
+// multiplied by: the smallest at which the largest magnitude of the 32 does not exceed e4m3's 448 (not floor(log2(amax)) - 8, at
+// which values up to an eighth beyond 448 would saturate).  The scaling is exact, so that a value's one rounding is the
+// code's, half a step of 2^-3 of it.  A value that is infinite or no number becomes the code for no number, alone.
+// Bound by HBM: 2 I elements in, I out, 2 I + I / 16 bytes of copy; the backward pass reads I elements and the copy and writes 2 I
+// elements (and the I of act, which the gradient of the next weights needs and which is not kept).  A thread has 8 columns of
+// gate and the same of up, four threads share an exponent by shuffles.
+
+#include <cuda_fp8.h>
+
+#include "rows_device.cuh"
+#include "sm100_device.cuh"
+
+namespace moe {
+namespace {
+
+constexpr int kActThreads = 256;
+
+struct GatedAct {
+    long long ld_in, ld_act, ld_d_act, ld_out;   // elements: gate_up, act, d_act, d_gate_up
+    uint8_t *codes, *scales;
+    int32_t rows, I, lanes;            // lanes: threads of a row, 4 per 32 columns
+    int32_t rows_per_cta;
+    Divisor by_lanes;
+};
+
+template <class E>
+__device__ __forceinline__ float exp_of(float x) { return sizeof(E) == 4 ? expf(x) : __expf(x); }
+// a / b; 16-bit results do not see the approximation's last bits (nor values below 2^-118, which it takes for zero)
+template <class E>
+__device__ __forceinline__ float ratio(float a, float b) { return sizeof(E) == 4 ? a / b : __fdividef(a, b); }
+
+// eight codes of x * 2^-e, x = 0 .. 448 * 2^e in magnitude
+__device__ __forceinline__ uint2 e4m3_codes(const float (&x)[8], int e, uint32_t bad)
+{
+    const float inv = power_of_two(-e);
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i] * inv, x[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2] * inv, x[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+        w[i] = lo | (hi << 16);
+    }
+    if (bad) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (bad >> i & 1u) w[i >> 2] |= 0x7Fu << (8 * (i & 3));
+    }
+    return make_uint2(w[0], w[1]);
+}
+// the exponent for a largest magnitude: smallest e >= -127 with amax <= 448 * 2^e = 1.75 * 2^(e + 8)
+__device__ __forceinline__ int e4m3_exponent(float amax)
+{
+    return max(-127, (int)((__float_as_uint(amax) + 0x1FFFFFu) >> 23) - 127 - 8);
+}
+__device__ __forceinline__ void e4m3_values(uint2 c, float scale, float (&x)[8])
+{
+    const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
+        const float2 f = __half22float2(__half2(h));
+        x[2 * i] = f.x * scale;
+        x[2 * i + 1] = f.y * scale;
+    }
+}
+
+template <class E, bool kKeep>
+__global__ void __launch_bounds__(kActThreads) gated_act_kernel(GatedAct p, const E *gate_up, E *act)
+{
+    grid_dependency_wait();
+    const long long row0 = (long long)blockIdx.x * p.rows_per_cta;
+    const int items = (int)min((long long)p.rows_per_cta, p.rows - row0) * p.lanes;
+    for (int base = (int)(threadIdx.x & ~31u); base < items; base += kActThreads) {
+        const int it = base + (int)(threadIdx.x & 31u), r = quotient(p.by_lanes, it), q = it - r * p.lanes;
+        const long long row = row0 + r;
+        const bool live = it < items && q * 8 < p.I;
+        float g[8], u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = u[i] = 0.0f;
+        if (live) {
+            const E *src = gate_up + row * p.ld_in + q * 8;
+            load8<E>(src, g);
+            load8<E>(src + p.I, u);
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = ratio<E>(g[i], 1.0f + exp_of<E>(-g[i])) * u[i];
+            store8<E>(act + row * p.ld_act + q * 8, y);
+        }
+        if (!kKeep) continue;
+        uint32_t bad_g, bad_u;
+        float mg = finite_amax8(g, bad_g), mu = finite_amax8(u, bad_u);
+#pragma unroll
+        for (int m = 1; m < 4; m *= 2) {
+            mg = fmaxf(mg, __shfl_xor_sync(0xffffffffu, mg, m));
+            mu = fmaxf(mu, __shfl_xor_sync(0xffffffffu, mu, m));
+        }
+        if (!live) continue;
+        const int eg = e4m3_exponent(mg), eu = e4m3_exponent(mu), blocks = p.lanes >> 2;
+        uint8_t *c = p.codes + row * 2 * p.I + q * 8;
+        *reinterpret_cast<uint2 *>(c) = e4m3_codes(g, eg, bad_g);
+        *reinterpret_cast<uint2 *>(c + p.I) = e4m3_codes(u, eu, bad_u);
+        if ((q & 3) == 0) {
+            uint8_t *sc = p.scales + row * 2 * blocks + (q >> 2);
+            sc[0] = (uint8_t)(eg + 127);
+            sc[blocks] = (uint8_t)(eu + 127);
+        }
+    }
+}
+
+template <class E>
+__global__ void __launch_bounds__(kActThreads) gated_act_grad_kernel(GatedAct p, const E *d_act, E *d_gate_up, E *act)
+{
+    grid_dependency_wait();
+    const long long row0 = (long long)blockIdx.x * p.rows_per_cta;
+    const int items = (int)min((long long)p.rows_per_cta, p.rows - row0) * p.lanes, blocks = p.lanes >> 2;
+    for (int it = (int)threadIdx.x; it < items; it += kActThreads) {
+        const int r = quotient(p.by_lanes, it), q = it - r * p.lanes;
+        if (q * 8 >= p.I) continue;
+        const long long row = row0 + r;
+        const uint8_t *c = p.codes + row * 2 * p.I + q * 8, *sc = p.scales + row * 2 * blocks + (q >> 2);
+        const uint2 cg = ld_row_v2(c), cu = ld_row_v2(c + p.I);
+        const float sg = power_of_two((int)ld_row_u8(sc) - 127), su = power_of_two((int)ld_row_u8(sc + blocks) - 127);
+        float d[8], g[8], u[8];
+        load8<E>(d_act + row * p.ld_d_act + q * 8, d);
+        e4m3_values(cg, sg, g);
+        e4m3_values(cu, su, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = ratio<E>(1.0f, 1.0f + exp_of<E>(-g[i])), silu = g[i] * s;
+            const float dg = d[i] * u[i] * (s * fmaf(g[i], 1.0f - s, 1.0f));
+            u[i] *= silu;                   // act
+            d[i] *= silu;                   // d_up
+            g[i] = dg;
+        }
+        E *dst = d_gate_up + row * p.ld_out + q * 8;
+        store8<E>(dst, g);
+        store8<E>(dst + p.I, d);
+        if (act) store8<E>(act + row * p.ld_act + q * 8, u);
+    }
+}
+
+bool sizes_ok(int32_t rows, int32_t I) { return rows >= 0 && rows < 1 << 30 && I >= 16 && I % 16 == 0 && I <= 1 << 20; }
+
+GatedAct describe(const moe_handle *h, int32_t rows, int32_t I)
+{
+    GatedAct p = {};
+    p.rows = rows;
+    p.I = I;
+    p.lanes = (I + 31) / 32 * 4;
+    p.by_lanes = divisor_of(p.lanes);
+    // 16 rows a block fill its passes of 256 threads to within a row; fewer where that leaves SMs without a block
+    p.rows_per_cta = 16;
+    while (p.rows_per_cta > 1 && (int64_t)rows < (int64_t)p.rows_per_cta * 4 * h->G) p.rows_per_cta /= 2;
+    return p;
+}
+
+}  // namespace
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" int32_t moe_gated_act(moe_handle *h, const void *gate_up, int64_t ld_gate_up, int32_t rows, int32_t I, int32_t dtype, void *act,
+                                 int64_t ld_act, void *codes_or_null, void *scales_or_null, void *stream)
+{
+    if (!h) return MOE_ERR_NULL;
+    if (!sizes_ok(rows, I)) return MOE_ERR_SHAPE;
+    if (!row_type_ok(dtype)) return MOE_ERR_UNSUPPORTED;
+    if (!pitch_ok(ld_gate_up, 2 * (int64_t)I) || !pitch_ok(ld_act, I)) return MOE_ERR_SHAPE;
+    if (rows == 0) return MOE_OK;
+    if (!gate_up || !act || !codes_or_null != !scales_or_null) return MOE_ERR_NULL;
+    if (!rows_aligned(gate_up) || !rows_aligned(act) || !rows_aligned(codes_or_null)) return MOE_ERR_ALIGN;
+    if (const int32_t rc = require_handle_device(h, "moe_gated_act")) return rc;
+    GatedAct p = describe(h, rows, I);
+    p.ld_in = ld_gate_up;
+    p.ld_act = ld_act;
+    p.codes = static_cast<uint8_t *>(codes_or_null);
+    p.scales = static_cast<uint8_t *>(scales_or_null);
+    const unsigned grid = (unsigned)((rows + p.rows_per_cta - 1) / p.rows_per_cta);
+    return with_row_type(dtype, [&](auto *e) -> int32_t {
+        using E = std::remove_pointer_t<decltype(e)>;
+        const E *in = static_cast<const E *>(gate_up);
+        E *out = static_cast<E *>(act);
+        const cudaError_t err = launch_chained(codes_or_null ? gated_act_kernel<E, true> : gated_act_kernel<E, false>, grid, kActThreads, 0,
+                                               static_cast<cudaStream_t>(stream), p, in, out);
+        return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "gated activation launch");
+    });
+}
+
+extern "C" int32_t moe_gated_act_grad(moe_handle *h, const void *d_act, int64_t ld_d_act, const void *codes, const void *scales, int32_t rows,
+                                      int32_t I, int32_t dtype, void *d_gate_up, int64_t ld_d_gate_up, void *act_or_null, int64_t ld_act, void *stream)
+{
+    if (!h) return MOE_ERR_NULL;
+    if (!sizes_ok(rows, I)) return MOE_ERR_SHAPE;
+    if (!row_type_ok(dtype)) return MOE_ERR_UNSUPPORTED;
+    if (!pitch_ok(ld_d_gate_up, 2 * (int64_t)I) || !pitch_ok(ld_d_act, I) || (act_or_null && !pitch_ok(ld_act, I))) return MOE_ERR_SHAPE;
+    if (rows == 0) return MOE_OK;
+    if (!d_act || !codes || !scales || !d_gate_up) return MOE_ERR_NULL;
+    if (!rows_aligned(d_act) || !rows_aligned(codes) || !rows_aligned(d_gate_up) || !rows_aligned(act_or_null)) return MOE_ERR_ALIGN;
+    if (const int32_t rc = require_handle_device(h, "moe_gated_act_grad")) return rc;
+    GatedAct p = describe(h, rows, I);
+    p.ld_act = ld_act;
+    p.ld_d_act = ld_d_act;
+    p.ld_out = ld_d_gate_up;
+    p.codes = static_cast<uint8_t *>(const_cast<void *>(codes));
+    p.scales = static_cast<uint8_t *>(const_cast<void *>(scales));
+    const unsigned grid = (unsigned)((rows + p.rows_per_cta - 1) / p.rows_per_cta);
+    return with_row_type(dtype, [&](auto *e) -> int32_t {
+        using E = std::remove_pointer_t<decltype(e)>;
+        const E *in = static_cast<const E *>(d_act);
+        E *out = static_cast<E *>(d_gate_up), *again = static_cast<E *>(act_or_null);
+        const cudaError_t err = launch_chained(gated_act_grad_kernel<E>, grid, kActThreads, 0, static_cast<cudaStream_t>(stream), p, in, out, again);
+        return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "gated activation gradient launch");
+    });
+}

@@ -267,6 +267,8 @@ const CUtensorMap *operand_map(moe_handle *h, const void *ptr, int32_t planes, i
 // ... of the gate and up weights [experts][2][inter][cols]: boxes of box_inter intermediate columns (a multiple of 16), in groups of 16
 // gate rows followed by the 16 up rows of the same columns; inter % 16 == 0
 const CUtensorMap *gate_up_map(moe_handle *h, const void *ptr, int32_t experts, int32_t inter, int32_t cols, int32_t box_inter, const char *name);
+// ... of rows of bytes (planes = 0: two dimensions), boxes of 128 bytes x box_rows, 128B swizzle; encoded anew by every call
+bool code_map(moe_handle *h, CUtensorMap *map, const void *ptr, int32_t planes, int64_t rows, int32_t row_bytes, int32_t box_rows, const char *name);
 // fused kernel (gemm2_combine.cu)
 size_t fused_smem_bytes(int tile_n);
 cudaError_t fused_occupancy(int tile_n, int *blocks_per_sm);
@@ -280,6 +282,8 @@ cudaError_t pair_occupancy(int *blocks_per_sm, int *max_clusters);
 cudaError_t pair_launch(const FusedParams &p, int grid, cudaStream_t stream);
 // GEMM1 (gemm1_act.cu): once per device, kernel attributes
 cudaError_t gemm1_prepare();
+// 4-bit product (mxfp4.cu): once per device, kernel attributes
+cudaError_t mxfp4_prepare();
 // moe_gemm1_act; mail_seq != 0: this launch mails the tile counts (with MOE_MTILES_ON_DEVICE); topk_idx != nullptr: it builds the
 // routing first
 int32_t launch_gemm1_act(moe_handle *h, const void *hidden, const void *W1, const int32_t *topk_idx, const moe_shape *s, int32_t tile_m,

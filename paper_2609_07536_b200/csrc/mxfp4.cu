@@ -1,0 +1,632 @@
+// Microscaled 4-bit floating point for the expert products: quantisation, its inverse, and the grouped product of routed rows
+// and expert weights that are both held in it.
+//
+// Format: a value is an e2m1 code (0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign) times 2^(e - 127), with one exponent byte e for 32 consecutive
+// columns: e - 127 = floor(log2(amax)) - 2, clamped to [-127, 127]; codes are rounded to the nearest, ties to even, and saturate at
+// 6.  A block with an infinity or no number gets e = 255, the code for no number, as a whole.
+// Codes lie [rows, K / 2], the even column in the low half of its byte.  Exponents lie as the tensor cores take them: blocks of
+// 128 rows x 128 columns are 512 bytes, row i, columns 32 s.. at 16 (i % 32) + 4 (i / 32) + s, so that the product copies them
+// from global memory through shared memory into TMEM as they are.  Rows come in groups (experts); row r of the group g whose rows
+// begin at o lies in row block o / 128 + g + (r - o) / 128: the blocks of two groups never meet, and no prefix over the groups is
+// needed to find them.
+
+#include <cuda_fp4.h>
+
+#include <cstring>
+
+#include "rows_device.cuh"
+#include "sm100_device.cuh"
+
+namespace moe {
+namespace {
+
+constexpr int kMxBlock = 32;           // columns that share an exponent
+constexpr int kMxTile = 128;           // rows and columns of an exponent block
+constexpr int kMxTileBytes = 512;
+
+// --------------------------------------------------------------------------- quantisation and back
+
+constexpr int kQuantThreads = 256;
+constexpr int kQuantRowsMax = 16, kQuantEntriesMax = kQuantRowsMax * 32;
+
+struct Quant {
+    const int32_t *offsets;        // [groups + 1], or nullptr: groups of n_even rows each
+    const int32_t *inv_perm;       // [src_rows, copies], or nullptr: row r from source row r
+    uint32_t *status;
+    uint8_t *codes, *scales;
+    long long ld, blocks;          // elements of the 16- or 32-bit matrix; row blocks of the exponents
+    int32_t rows, src_rows, copies, groups, n_even;
+    int32_t K, KQ, lanes, rows_per_cta;   // KQ = ceil(K / 128); lanes: threads of a row, 16 per 128 columns
+    Divisor by_lanes, by_copies, by_n;
+};
+struct QuantRow {
+    int32_t r;                     // row of the codes, -1: none
+    long long at;                  // its first exponent byte
+};
+
+// Where row `r` lies; rows behind the last group have no place
+__device__ __forceinline__ QuantRow quant_row(const Quant &p, int r, uint32_t what)
+{
+    QuantRow q = {-1, 0};
+    if (r < 0) return q;
+    int g, o;
+    if (p.offsets) {
+        if (r >= ld_chained(p.offsets + p.groups)) return q;
+        int lo = 0, hi = p.groups - 1;         // the last group that begins at or before r: the one with rows among equals
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (ld_chained(p.offsets + mid) <= r) lo = mid;
+            else hi = mid - 1;
+        }
+        g = lo;
+        o = ld_chained(p.offsets + g);
+    } else {
+        g = quotient(p.by_n, r);
+        o = g * p.n_even;
+    }
+    const int i = r - o;
+    const long long block = (long long)(o / kMxTile) + g + i / kMxTile;
+    if (o < 0 || i < 0 || block >= p.blocks) {
+        report(p.status, MOE_DEV_OOB, what, 62u);
+        return q;
+    }
+    q.r = r;
+    q.at = block * p.KQ * kMxTileBytes + (i & 31) * 16 + ((i & 127) >> 5) * 4;
+    return q;
+}
+
+// e2m1 codes of eight values times `inv`, the first in the lowest four bits
+__device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], float inv)
+{
+    uint32_t w = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(x[2 * i] * inv, x[2 * i + 1] * inv), __NV_E2M1, cudaRoundNearest) << (8 * i);
+    return w;
+}
+
+template <class E, bool kGather>
+__global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const __grid_constant__ Quant p, const E *src)
+{
+    __shared__ QuantRow where[kQuantEntriesMax];
+    grid_dependency_wait();
+    const int row0 = (int)blockIdx.x * p.rows_per_cta, n = min(p.rows_per_cta, p.src_rows - row0);
+    for (int i = threadIdx.x; i < n * p.copies; i += kQuantThreads) {
+        if (kGather) {
+            const long long f = (long long)row0 * p.copies + i;
+            int r = ld_chained(p.inv_perm + f);
+            if (r < -1 || r >= p.rows) {
+                report(p.status, MOE_DEV_OOB, (uint32_t)f, 61u);
+                r = -1;
+            }
+            where[i] = quant_row(p, r, (uint32_t)f);
+        } else {
+            where[i] = quant_row(p, row0 + i, (uint32_t)(row0 + i));
+        }
+    }
+    __syncthreads();
+    const int items = n * p.lanes;
+    for (int base = (int)(threadIdx.x & ~31u); base < items; base += kQuantThreads) {
+        const int it = base + (int)(threadIdx.x & 31u), i = quotient(p.by_lanes, it), q = it - i * p.lanes;
+        const bool in = it < items, live = in && q * 8 < p.K;
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = 0.0f;
+        if (live) load8<E>(src + (long long)(row0 + i) * p.ld + q * 8, x);
+        uint32_t bad;
+        float amax = finite_amax8(x, bad);
+        if (bad) amax = __uint_as_float(0x7f800000u);
+#pragma unroll
+        for (int m = 1; m < 4; m *= 2) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
+        // floor(log2(amax)) - 2, biased: the exponent field less 2; 255: no number
+        const int field = (int)(__float_as_uint(amax) >> 23), e = field == 255 ? 255 : max(0, field - 2);
+        const uint32_t codes = field == 255 ? 0u : e2m1_codes(x, power_of_two(127 - e));
+        uint32_t bytes = live ? (uint32_t)e << (8 * ((q >> 2) & 3)) : 0u;
+#pragma unroll
+        for (int m = 4; m < 16; m *= 2) bytes |= __shfl_xor_sync(0xffffffffu, bytes, m);
+        if (!in) continue;
+        for (int j = 0; j < (kGather ? p.copies : 1); ++j) {
+            const QuantRow w = where[kGather ? i * p.copies + j : i];
+            if (w.r < 0) continue;
+            if (live) *reinterpret_cast<uint32_t *>(p.codes + (long long)w.r * (p.K / 2) + q * 4) = codes;
+            if ((q & 15) == 0) *reinterpret_cast<uint32_t *>(p.scales + w.at + (long long)(q >> 4) * kMxTileBytes) = bytes;
+        }
+    }
+}
+
+template <class E>
+__global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_constant__ Quant p, E *dst)
+{
+    __shared__ QuantRow where[kQuantRowsMax];
+    grid_dependency_wait();
+    const int row0 = (int)blockIdx.x * p.rows_per_cta, n = min(p.rows_per_cta, p.rows - row0);
+    if ((int)threadIdx.x < n) where[threadIdx.x] = quant_row(p, row0 + (int)threadIdx.x, (uint32_t)(row0 + (int)threadIdx.x));
+    __syncthreads();
+    const int items = n * p.lanes;
+    for (int it = (int)threadIdx.x; it < items; it += kQuantThreads) {
+        const int i = quotient(p.by_lanes, it), q = it - i * p.lanes;
+        const QuantRow w = where[i];
+        if (w.r < 0 || q * 8 >= p.K) continue;
+        const uint32_t c = ld_row_u32(p.codes + (long long)w.r * (p.K / 2) + q * 4);
+        const int e = (int)ld_row_u8(p.scales + w.at + (long long)(q >> 4) * kMxTileBytes + ((q >> 2) & 3));
+        const float scale = e == 255 ? __uint_as_float(0x7fffffffu) : power_of_two(e - 127);
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(c >> (8 * k)), __NV_E2M1);
+            const float2 f = __half22float2(__half2(h));
+            x[2 * k] = f.x * scale;
+            x[2 * k + 1] = f.y * scale;
+        }
+        store8<E>(dst + (long long)w.r * p.ld + q * 8, x);
+    }
+}
+
+// --------------------------------------------------------------------------- grouped product
+//
+// out[r][n] = sum_k x[r][k] w[e][n][k] for the rows r of expert e, fp32 accumulation in TMEM, one rounding at the end.
+// The weights are on the M side of the MMA and the rows on its N side, as in the other products here: a tile costs what its rows cost.
+// Tile: 128 columns of the output x up to 192 rows.  TMEM holds two accumulators of 192 columns and, for every operand stage, 24
+// columns of exponents (128 rows of weights: 4 per 128 columns of K; 256 rows of x: 8); that is 504 of its 512 columns, and why a
+// tile has 192 rows and not 256.  A stage is 256 columns of K: 128 bytes of codes a row, a swizzle row.
+//   warp 0      TMA producer (one thread): codes of weights and rows, and their exponents as they lie;
+//   warp 1      copies the exponents to TMEM (tcgen05.cp, each of the four lane quarters gets them) and issues
+//               tcgen05.mma.kind::mxf4.block_scale (K = 64, two exponents a row); both are issued by one lane of the converged
+//               warp and run in order;
+//   warps 4-11  epilogue: pieces of 32 rows x 32 columns, 16-bit, transposed in registers, 64 contiguous bytes a row.
+
+constexpr int kPrThreads = 384, kPrEpiWarps = 8;
+constexpr int kPrN = 128;                                   // output columns of a tile (M of the MMA)
+constexpr int kPrRows = 192;                                // rows of a tile (N of the MMA)
+constexpr int kPrK = 256, kPrStepK = 64;                    // columns of K of a stage, of an MMA
+constexpr int kPrBoxRows = 64;                              // rows that one copy of x brings
+constexpr int kPrStages = 5;
+constexpr int kPrWBytes = kPrN * kPrK / 2, kPrXBytes = kPrRows * kPrK / 2;
+constexpr int kPrWScaleBytes = 2 * kMxTileBytes, kPrXScaleBytes = 4 * kMxTileBytes;      // x: row block 0 of both 128s of K, then row block 1
+constexpr int kPrStageBytes = kPrWBytes + kPrXBytes + kPrWScaleBytes + kPrXScaleBytes;
+constexpr int kPrScaleCols = 24;                            // TMEM columns of a stage's exponents: weights 2 x 4, rows 2 x 8
+constexpr int kPrTmemCols = 512;
+constexpr int kMaxExperts = 1024;
+static_assert(2 * kPrRows + kPrStages * kPrScaleCols <= kPrTmemCols, "accumulators and exponents exceed TMEM");
+static_assert(kPrStageBytes % 1024 == 0, "stages are 1024-byte aligned");
+
+struct alignas(64) ProductParams {
+    CUtensorMap tmW;   // codes [E][N][K / 2]   box 128 bytes x 128 rows, 128B swizzle
+    CUtensorMap tmX;   // codes [R][K / 2]      box 128 bytes x 64 rows
+    const uint8_t *w_scales, *x_scales;
+    const int32_t *offsets;        // [E + 1]
+    void *out;
+    long long ld_out;              // elements
+    uint32_t *status;
+    unsigned long long wait_ns;
+    int32_t R, E, N, KQ, num_kb, last_steps, NT;
+    Divisor by_NT;
+};
+struct ProductControl {
+    unsigned long long full[kPrStages], empty[kPrStages], tmem_full[2], tmem_empty[2], drain;
+    uint32_t tmem_base;
+    volatile uint32_t abort;
+    int32_t first[kMaxExperts + 1];       // row where an expert's rows begin
+    int32_t tiles[kMaxExperts + 1];       // row tiles of the experts before
+};
+
+__device__ __forceinline__ bool pr_wait(uint32_t bar, uint32_t parity, ProductControl *ctl, unsigned long long deadline, uint32_t *status,
+                                        uint32_t detail, uint32_t where)
+{
+    uint32_t spins = 0;
+    while (!mbar_try_wait(bar, parity)) {
+        if ((++spins & 63u) == 0u) {
+            if (ctl->abort) return false;
+            if (globaltimer_ns() > deadline) {
+                ctl->abort = 1u;
+                report(status, MOE_DEV_TIMEOUT, detail, where);
+                return false;
+            }
+        }
+    }
+    return true;
+}
+
+struct ProductTile {
+    int e, row0, valid, local, n0;     // local: first row inside the expert
+};
+__device__ __forceinline__ ProductTile pr_tile(int g, const ProductParams &P, const ProductControl *ctl)
+{
+    const int mu = quotient(P.by_NT, g);
+    int lo = 0, hi = P.E - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (ctl->tiles[mid] <= mu) lo = mid;
+        else hi = mid - 1;
+    }
+    ProductTile t;
+    t.e = lo;
+    t.local = (mu - ctl->tiles[lo]) * kPrRows;
+    t.row0 = ctl->first[lo] + t.local;
+    t.valid = min(kPrRows, ctl->first[lo + 1] - t.row0);
+    t.n0 = (g - mu * P.NT) * kPrN;
+    return t;
+}
+
+// Instruction descriptor, kind::mxf4: e2m1 operands, K-major, M = 128, exponents of type ue8m0, exponent pair `half` of the column's four bytes
+__device__ __forceinline__ uint32_t mxf4_idesc(uint32_t n, uint32_t half)
+{
+    return (2u * half << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((uint32_t)(kPrN >> 4) << 24) | (2u * half << 29);
+}
+__device__ __forceinline__ void tc_mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t a_scale, uint32_t b_scale,
+                                            uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+        : "memory");
+}
+// 32 rows of 16 bytes of shared memory (512 contiguous bytes) -> 32 lanes x 4 columns of TMEM, in each of the four lane quarters
+__device__ __forceinline__ void tc_cp_scales(uint32_t d_tmem, uint32_t smem)
+{
+    // no swizzle; eights of rows 128 bytes apart (stride offset); version 1
+    const uint64_t desc = ((uint64_t)((128u >> 4) | (1u << 14)) << 32) | ((smem & 0x3FFFFu) >> 4) | (1u << 16);
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(d_tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"((unsigned long long)map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
+// 32 rows x 32 columns of an accumulator -> 16 bits, one store instruction 64 contiguous bytes of eight rows.  `dst`: lane i, where the
+// first of the columns of row i goes (nullptr: nowhere); `cols`: columns that exist (a multiple of 8)
+template <class E>
+__device__ __forceinline__ void store_piece(const uint32_t (&lo)[16], const uint32_t (&hi)[16], E *dst, int cols)
+{
+    const int lane = threadIdx.x & 31, c = lane & 3;
+    const auto pack = [](uint32_t a, uint32_t b) { return RowType<E>::pack(__uint_as_float(a), __uint_as_float(b)); };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {                // rows 8j..8j+7; this lane: row 8j + lane / 4
+        uint32_t v[4] = {transpose_8x8(pack(lo[4 * j], lo[4 * j + 1])), transpose_8x8(pack(lo[4 * j + 2], lo[4 * j + 3])),
+                         transpose_8x8(pack(hi[4 * j], hi[4 * j + 1])), transpose_8x8(pack(hi[4 * j + 2], hi[4 * j + 3]))};
+        // v[m]: columns 8m + 2c and the next one -> v[k]: columns 8c + 2k and the next one
+#pragma unroll
+        for (int d = 1; d < 4; d *= 2)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                if (m & d) continue;
+                const bool up = (c & d) != 0;
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? v[m] : v[m + d], d);
+                if (up) v[m] = got;
+                else v[m + d] = got;
+            }
+        E *row = reinterpret_cast<E *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), 8 * j + (lane >> 2)));
+        if (row != nullptr && c * 8 < cols) st_row_v4(row + c * 8, make_uint4(v[0], v[1], v[2], v[3]));
+    }
+}
+
+template <class E>
+__global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __grid_constant__ ProductParams P)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    ProductControl *ctl = reinterpret_cast<ProductControl *>(ring + kPrStages * kPrStageBytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPrStages; ++i) {
+            mbar_init(smem_u32(&ctl->full[i]), 1);
+            mbar_init(smem_u32(&ctl->empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&ctl->tmem_full[i]), 1);
+            mbar_init(smem_u32(&ctl->tmem_empty[i]), kPrEpiWarps);
+        }
+        mbar_init(smem_u32(&ctl->drain), 1);
+        ctl->abort = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        prefetch_tensormap(&P.tmW);
+        prefetch_tensormap(&P.tmX);
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&ctl->tmem_base), kPrTmemCols);
+    grid_dependency_wait();
+    if (warp == 2) {
+        // where the experts' rows begin and how many row tiles lie before them; what is out of range is reported and has no rows
+        int tiles = 0, before = 0;
+        for (int e0 = 0; e0 <= P.E; e0 += 32) {
+            const int e = e0 + lane;
+            const int raw = ld_chained(P.offsets + min(e, P.E));
+            int o = min(max(raw, before), P.R);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {                     // running maximum: offsets never go back
+                const int u = __shfl_up_sync(0xffffffffu, o, d);
+                if (lane >= d) o = max(o, u);
+            }
+            if (e <= P.E && o != raw && blockIdx.x == 0) report(P.status, MOE_DEV_OOB, (uint32_t)e, 63u);
+            int prev = __shfl_up_sync(0xffffffffu, o, 1);
+            if (lane == 0) prev = before;
+            // row tiles of the expert that ends at `o` (expert e - 1)
+            int t = (e > 0 && e <= P.E) ? (o - prev + kPrRows - 1) / kPrRows : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, t, d);
+                if (lane >= d) t += u;
+            }
+            if (e <= P.E) {
+                ctl->first[e] = o;
+                ctl->tiles[e] = tiles + t;
+            }
+            before = __shfl_sync(0xffffffffu, o, 31);
+            tiles += __shfl_sync(0xffffffffu, t, 31);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+    const int total = ctl->tiles[P.E] * P.NT, stride = (int)gridDim.x;
+    const unsigned long long deadline = globaltimer_ns() + P.wait_ns;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0, armed = 0;
+            bool ok = true;
+            for (int g = (int)blockIdx.x; g < total && ok; g += stride) {
+                const ProductTile t = pr_tile(g, P, ctl);
+                const int boxes = (t.valid + kPrBoxRows - 1) / kPrBoxRows;
+                const int shift = t.local & (kMxTile - 1);                     // 0 or 64: first row inside its exponent block
+                const int xblocks = shift + t.valid > kMxTile ? 2 : 1;
+                const long long row_bytes = (long long)P.KQ * kMxTileBytes;
+                // the offset that the quantisation used: the expert's first row (t.row0 - t.local)
+                const uint8_t *xs = P.x_scales + ((long long)((t.row0 - t.local) / kMxTile) + t.e + t.local / kMxTile) * row_bytes;
+                const uint8_t *ws = P.w_scales + ((long long)t.e * P.N / kMxTile + t.e + t.n0 / kMxTile) * row_bytes;
+                for (int kb = 0; kb < P.num_kb; ++kb) {
+                    ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)g, 70u);
+                    if (!ok) break;
+                    const uint32_t bar = smem_u32(&ctl->full[stage]), w_dst = smem_u32(ring + stage * kPrStageBytes);
+                    const uint32_t x_dst = w_dst + kPrWBytes, ws_dst = x_dst + kPrXBytes, xs_dst = ws_dst + kPrWScaleBytes;
+                    const uint32_t sb = (uint32_t)min(2, P.KQ - 2 * kb) * kMxTileBytes;      // exponents of a row block
+                    mbar_arrive_expect_tx(bar, kPrWBytes + (uint32_t)boxes * (kPrBoxRows * kPrK / 2) + sb * (1u + (uint32_t)xblocks));
+                    tma_load_3d(w_dst, &P.tmW, bar, kb * (kPrK / 2), t.n0, t.e);
+                    for (int b = 0; b < boxes; ++b)
+                        tma_load_2d(x_dst + (uint32_t)b * (kPrBoxRows * kPrK / 2), &P.tmX, bar, kb * (kPrK / 2), t.row0 + b * kPrBoxRows);
+                    bulk_load(ws_dst, ws + kb * (2 * kMxTileBytes), sb, bar);
+                    for (int b = 0; b < xblocks; ++b)
+                        bulk_load(xs_dst + (uint32_t)b * (2 * kMxTileBytes), xs + b * row_bytes + kb * (2 * kMxTileBytes), sb, bar);
+                    armed |= 1u << stage;
+                    if (++stage == kPrStages) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok) {
+                // wind-down: let the copies already issued land before shared memory is released
+                const unsigned long long drain = globaltimer_ns() + 2000000ull;
+                for (int i = 0; i < kPrStages; ++i) {
+                    if (!(armed & (1u << i))) continue;
+                    const uint32_t par = i < stage ? phase : (phase ^ 1u);
+                    while (!mbar_try_wait(smem_u32(&ctl->full[i]), par) && globaltimer_ns() < drain) {}
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        int stage = 0, it = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int g = (int)blockIdx.x; g < total && ok; g += stride, ++it) {
+            const ProductTile t = pr_tile(g, P, ctl);
+            const int a = it & 1, shift = t.local & (kMxTile - 1), xblocks = shift + t.valid > kMxTile ? 2 : 1;
+            const uint32_t n = (uint32_t)((t.valid + 15) & ~15), idesc0 = mxf4_idesc(n, 0u), idesc1 = mxf4_idesc(n, 1u);
+            ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), ((uint32_t)(it >> 1) & 1u) ^ 1u, ctl, deadline, P.status, (uint32_t)g, 71u));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t d_tmem = tmem_base + (uint32_t)(a * kPrRows);
+            for (int kb = 0; kb < P.num_kb; ++kb) {
+                ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->full[stage]), phase, ctl, deadline, P.status, (uint32_t)g, 72u));
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one_sync()) {
+                    const uint32_t w = smem_u32(ring + stage * kPrStageBytes), x = w + kPrWBytes, ws = x + kPrXBytes, xs = ws + kPrWScaleBytes;
+                    const uint32_t sw = tmem_base + (uint32_t)(2 * kPrRows + stage * kPrScaleCols), sx = sw + 8u;
+                    const int steps = kb == P.num_kb - 1 ? P.last_steps : kPrK / kPrStepK, quarters = (steps + 1) >> 1;
+                    for (int q = 0; q < quarters; ++q) {
+                        tc_cp_scales(sw + 4u * q, ws + q * kMxTileBytes);
+                        for (int b = 0; b < xblocks; ++b) tc_cp_scales(sx + 8u * q + 4u * b, xs + (2 * b + q) * kMxTileBytes);
+                    }
+                    const uint64_t wd = ((uint64_t)kSmemDescHi << 32) | smem_desc_lo(w), xd = ((uint64_t)kSmemDescHi << 32) | smem_desc_lo(x);
+                    for (int k = 0; k < steps; ++k)
+                        tc_mma_mxf4(d_tmem, wd + (uint64_t)(2 * k), xd + (uint64_t)(2 * k), k & 1 ? idesc1 : idesc0, sw + 4u * (k >> 1),
+                                    sx + 8u * (k >> 1) + (uint32_t)(shift >> 5), (k > 0 || kb > 0) ? 1u : 0u);
+                    tc_commit(smem_u32(&ctl->empty[stage]));
+                    if (kb == P.num_kb - 1) tc_commit(smem_u32(&ctl->tmem_full[a]));
+                }
+                __syncwarp();
+                if (++stage == kPrStages) { stage = 0; phase ^= 1u; }
+            }
+        }
+        if (!ok) {
+            // what was issued finishes before shared memory and TMEM are released
+            if (elect_one_sync()) tc_commit(smem_u32(&ctl->drain));
+            __syncwarp();
+            const unsigned long long until = globaltimer_ns() + 2000000ull;
+            while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < until) {}
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        const int q4 = warp & 3, grp = (warp - 4) >> 2;
+        int it = 0;
+        for (int g = (int)blockIdx.x; g < total; g += stride, ++it) {
+            const ProductTile t = pr_tile(g, P, ctl);
+            const int a = it & 1, pieces = (t.valid + 31) >> 5, col = t.n0 + q4 * 32, cols = P.N - col;
+            uint32_t ok = 1u;
+            if (lane == 0) ok = pr_wait(smem_u32(&ctl->tmem_full[a]), (uint32_t)(it >> 1) & 1u, ctl, deadline, P.status, (uint32_t)g, 73u) ? 1u : 0u;
+            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+            tc_fence_after();
+            const uint32_t taddr = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(a * kPrRows);
+            const auto release = [&]() {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl->tmem_empty[a]));
+            };
+            if (grp >= pieces) release();
+#pragma unroll 1
+            for (int piece = grp; piece < pieces; piece += kPrEpiWarps / 4) {
+                uint32_t lo[16], hi[16];
+                tmem_ld_16x256_x4(taddr + (uint32_t)(piece * 32), lo);
+                tmem_ld_16x256_x4(taddr + (16u << 16) + (uint32_t)(piece * 32), hi);
+                tmem_ld_wait(lo);
+                tmem_ld_wait(hi);
+                if (piece + kPrEpiWarps / 4 >= pieces) release();
+                const int row = piece * 32 + lane;
+                E *dst = row < t.valid && cols > 0 ? static_cast<E *>(P.out) + (long long)(t.row0 + row) * P.ld_out + col : nullptr;
+                store_piece<E>(lo, hi, dst, cols);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, kPrTmemCols);
+    }
+}
+
+constexpr size_t kPrSmem = (size_t)kPrStages * kPrStageBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127);
+static_assert(kPrSmem <= 227 * 1024, "the product's stages exceed the shared memory of an SM");
+
+bool columns_ok(int32_t K) { return K >= kMxBlock && K % kMxBlock == 0 && K <= 1 << 20; }
+int64_t scale_blocks(int64_t rows, int32_t groups) { return rows / kMxTile + groups; }
+
+int32_t describe(moe_handle *h, const char *who, int32_t rows, int32_t src_rows, int32_t copies, int32_t K, int32_t groups, int32_t dtype, int64_t ld,
+                 const int32_t *offsets, const int32_t *inv_perm, const void *matrix, const void *codes, const void *scales, uint32_t *status, Quant *p)
+{
+    if (!h || !status) return MOE_ERR_NULL;
+    if (rows < 0 || rows >= 1 << 30 || groups < 1 || groups > (1 << 20) || !columns_ok(K) || !pitch_ok(ld, K)) return MOE_ERR_SHAPE;
+    if (!offsets && rows % groups != 0) return MOE_ERR_SHAPE;
+    if (!row_type_ok(dtype)) return MOE_ERR_UNSUPPORTED;
+    p->rows = 0;
+    if (rows == 0) return MOE_OK;
+    if (!matrix || !codes || !scales) return MOE_ERR_NULL;
+    if (!rows_aligned(matrix) || !rows_aligned(codes) || !rows_aligned(scales) || !rows_aligned(status)) return MOE_ERR_ALIGN;
+    if (const int32_t rc = require_handle_device(h, who)) return rc;
+    memset(p, 0, sizeof *p);
+    p->codes = static_cast<uint8_t *>(const_cast<void *>(codes));
+    p->scales = static_cast<uint8_t *>(const_cast<void *>(scales));
+    p->offsets = offsets;
+    p->inv_perm = inv_perm;
+    p->status = status;
+    p->ld = ld;
+    p->blocks = scale_blocks(rows, groups);
+    p->rows = rows;
+    p->src_rows = src_rows;
+    p->copies = copies;
+    p->groups = groups;
+    p->n_even = rows / groups > 0 ? rows / groups : 1;
+    p->K = K;
+    p->KQ = (K + kMxTile - 1) / kMxTile;
+    p->lanes = p->KQ * 16;
+    p->by_lanes = divisor_of(p->lanes);
+    p->by_n = divisor_of(p->n_even);
+    p->rows_per_cta = kQuantRowsMax;
+    while (p->rows_per_cta > 1 && (int64_t)src_rows < (int64_t)p->rows_per_cta * 4 * h->G) p->rows_per_cta /= 2;
+    return MOE_OK;
+}
+
+}  // namespace
+}  // namespace moe
+
+using namespace moe;
+
+cudaError_t moe::mxfp4_prepare()
+{
+    cudaError_t e = cudaFuncSetAttribute(mxfp4_product_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPrSmem);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(mxfp4_product_kernel<__half>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPrSmem);
+}
+
+extern "C" int32_t moe_mxfp4_scale_bytes(int32_t rows, int32_t K, int32_t groups, size_t *bytes)
+{
+    if (!bytes) return MOE_ERR_NULL;
+    if (rows < 0 || rows >= 1 << 30 || groups < 1 || groups > 1 << 20 || !columns_ok(K)) return MOE_ERR_SHAPE;
+    *bytes = (size_t)scale_blocks(rows, groups) * (size_t)((K + kMxTile - 1) / kMxTile) * kMxTileBytes;
+    return MOE_OK;
+}
+
+extern "C" int32_t moe_mxfp4_quantize(moe_handle *h, const void *src, int64_t ld_src, int32_t dtype, int32_t rows, int32_t K, int32_t groups,
+                                      const int32_t *offsets_or_null, const int32_t *inv_perm_or_null, int32_t copies, void *codes, void *scales,
+                                      uint32_t *status_dev, void *stream)
+{
+    if (inv_perm_or_null ? copies < 1 || copies > 32 || rows % copies != 0 : copies != 1) return MOE_ERR_SHAPE;
+    Quant p;
+    const int32_t rc = describe(h, "moe_mxfp4_quantize", rows, rows / copies, copies, K, groups, dtype, ld_src, offsets_or_null, inv_perm_or_null, src, codes, scales,
+                                status_dev, &p);
+    if (rc != MOE_OK || p.rows == 0) return rc;
+    const unsigned grid = (unsigned)((p.src_rows + p.rows_per_cta - 1) / p.rows_per_cta);
+    return with_row_type(dtype, [&](auto *e) -> int32_t {
+        using E = std::remove_pointer_t<decltype(e)>;
+        const cudaError_t err = launch_chained(inv_perm_or_null ? quantize_kernel<E, true> : quantize_kernel<E, false>, grid, kQuantThreads, 0,
+                                               static_cast<cudaStream_t>(stream), p, static_cast<const E *>(src));
+        return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "quantisation launch");
+    });
+}
+
+extern "C" int32_t moe_mxfp4_dequantize(moe_handle *h, const void *codes, const void *scales, int32_t rows, int32_t K, int32_t groups,
+                                        const int32_t *offsets_or_null, int32_t dtype, void *out, int64_t ld_out, uint32_t *status_dev, void *stream)
+{
+    Quant p;
+    const int32_t rc = describe(h, "moe_mxfp4_dequantize", rows, rows, 1, K, groups, dtype, ld_out, offsets_or_null, nullptr, out, codes, scales, status_dev, &p);
+    if (rc != MOE_OK || p.rows == 0) return rc;
+    const unsigned grid = (unsigned)((rows + p.rows_per_cta - 1) / p.rows_per_cta);
+    return with_row_type(dtype, [&](auto *e) -> int32_t {
+        using E = std::remove_pointer_t<decltype(e)>;
+        const cudaError_t err = launch_chained(dequantize_kernel<E>, grid, kQuantThreads, 0, static_cast<cudaStream_t>(stream), p, static_cast<E *>(out));
+        return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "dequantisation launch");
+    });
+}
+
+extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void *x_scales, const void *w_codes, const void *w_scales,
+                                  const int32_t *offsets, int32_t rows, int32_t E_tot, int32_t N, int32_t K, int32_t dtype, void *out, int64_t ld_out,
+                                  uint32_t *status_dev, void *stream)
+{
+    if (!h || !status_dev) return MOE_ERR_NULL;
+    if (rows < 0 || rows >= 1 << 30 || E_tot < 1 || E_tot > kMaxExperts || N < 8 || N % 8 != 0 || (int64_t)E_tot * N >= 1 << 30 || !columns_ok(K) ||
+        !pitch_ok(ld_out, N))
+        return MOE_ERR_SHAPE;
+    if (dtype != MOE_BF16 && dtype != MOE_FP16) return MOE_ERR_UNSUPPORTED;
+    if (rows == 0) return MOE_OK;
+    if (!x_codes || !x_scales || !w_codes || !w_scales || !offsets || !out) return MOE_ERR_NULL;
+    if (!rows_aligned(x_codes) || !rows_aligned(x_scales) || !rows_aligned(w_codes) || !rows_aligned(w_scales) || !rows_aligned(out) ||
+        !rows_aligned(status_dev))
+        return MOE_ERR_ALIGN;
+    if (const int32_t rc = require_handle_device(h, "moe_mxfp4_gemm")) return rc;
+    ProductParams p;
+    memset(&p, 0, sizeof p);
+    p.w_scales = static_cast<const uint8_t *>(w_scales);
+    p.x_scales = static_cast<const uint8_t *>(x_scales);
+    p.offsets = offsets;
+    p.out = out;
+    p.ld_out = ld_out;
+    p.status = status_dev;
+    p.wait_ns = h->wait_ns;
+    p.R = rows;
+    p.E = E_tot;
+    p.N = N;
+    p.KQ = (K + kMxTile - 1) / kMxTile;
+    p.num_kb = (K + kPrK - 1) / kPrK;
+    p.last_steps = (K - (p.num_kb - 1) * kPrK + kPrStepK - 1) / kPrStepK;
+    p.NT = (N + kPrN - 1) / kPrN;
+    p.by_NT = divisor_of(p.NT);
+    const int64_t used = rows < E_tot ? rows : E_tot, tiles = ((rows - used) / kPrRows + used) * p.NT;      // at most
+    if (tiles >= (int64_t)1 << 31) return MOE_ERR_SHAPE;
+    if (!code_map(h, &p.tmW, w_codes, E_tot, N, K / 2, kPrN, "w_codes") || !code_map(h, &p.tmX, x_codes, 0, rows, K / 2, kPrBoxRows, "x_codes"))
+        return MOE_ERR_CUDA;
+    const unsigned grid = (unsigned)(tiles < h->G ? tiles : h->G);
+    const cudaError_t err = launch_chained(dtype == MOE_BF16 ? mxfp4_product_kernel<__nv_bfloat16> : mxfp4_product_kernel<__half>, grid, kPrThreads, kPrSmem,
+                                           static_cast<cudaStream_t>(stream), p);
+    return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "grouped 4-bit product launch");
+}
