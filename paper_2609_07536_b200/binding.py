@@ -423,53 +423,68 @@ def moe_layer_host(h, x_routed_host, topk_idx_host, topk_w_host, W2_dev, shape, 
 # These take their sizes, element type and row distance from the tensors, and refuse tensors that do not fit together with the
 # status code that the library has for it.
 
-_types = {}
+# A decode step's kernel is shorter than the call that launches it, so the checks look at the usual case first, in one
+# condition, and at what is wrong only where it does not hold.
 
-
-def _row_type(t, who):
-    if not _types:
-        import torch
-        _types.update({torch.bfloat16: MOE_BF16, torch.float16: MOE_FP16, torch.float32: MOE_FP32})
-    code = _types.get(t.dtype)
-    if code is None:
-        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"element type {t.dtype}")
-    return code
-
-
-def _on_device(h_device, t, who, what):
-    if t.get_device() != h_device:
-        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is on {t.device}, the current CUDA device is {h_device}")
-
-
-def _matrix(t, rows, cols, like, device, who, what):
-    """(address, row distance) of a matrix of at least `rows` x exactly `cols` with contiguous columns."""
-    shape = t.shape
-    if len(shape) != 2 or shape[0] < rows or shape[1] != cols:
-        raise MoeError(MOE_ERR_SHAPE, who, f"{what} is {tuple(shape)}, not [{rows}, {cols}]")
-    if t.dtype != like:
-        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is {t.dtype}, not {like}")
-    _on_device(device, t, who, what)
-    ld, one = t.stride()
-    if one != 1 and cols > 1:
-        raise MoeError(MOE_ERR_SHAPE, who, f"the columns of {what} are not contiguous")
-    return t.data_ptr(), ld if shape[0] > 1 else max(ld, cols) if ld % 8 == 0 else cols
-
-
-def _vector(t, n, kind, device, who, what):
-    """Address of `n` contiguous elements of torch type `kind` (a raw address, or None, is passed on)."""
-    if t is None or isinstance(t, int):
-        return t
-    if str(t.dtype) != kind:
-        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is {t.dtype}, not {kind}")
-    if t.numel() < n or not t.is_contiguous():
-        raise MoeError(MOE_ERR_SHAPE, who, f"{what} is not {n} contiguous elements")
-    _on_device(device, t, who, what)
-    return t.data_ptr()
+_types = {}          # torch element type -> the library's
+_i32 = _u8 = _f32 = None
+_current_raw_stream = None
 
 
 def _device():
+    """The calling thread's current CUDA device (the first call fills the tables of element types)."""
     import torch
+    if not _types:
+        global _i32, _u8, _f32, _current_raw_stream
+        _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _i32, _u8, _f32 = torch.int32, torch.uint8, torch.float32
+        _types.update({torch.bfloat16: MOE_BF16, torch.float16: MOE_FP16, torch.float32: MOE_FP32})
     return torch.cuda.current_device()
+
+
+def _row_type(kind, who):
+    code = _types.get(kind)
+    if code is None:
+        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"element type {kind}")
+    return code
+
+
+def _matrix(t, rows, cols, kind, device, who, what):
+    """(address, row distance) of a matrix of at least `rows` x exactly `cols` with contiguous columns."""
+    shape = t.shape
+    if len(shape) == 2 and shape[0] >= rows and shape[1] == cols and t.dtype is kind and t.get_device() == device:
+        if t.is_contiguous():
+            return t.data_ptr(), cols
+        ld, one = t.stride()
+        if one == 1 and shape[0] > 1:
+            return t.data_ptr(), ld
+        raise MoeError(MOE_ERR_SHAPE, who, f"the columns of {what} are not contiguous")
+    if len(shape) != 2 or shape[0] < rows or shape[1] != cols:
+        raise MoeError(MOE_ERR_SHAPE, who, f"{what} is {tuple(shape)}, not [{rows}, {cols}]")
+    if t.dtype is not kind:
+        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is {t.dtype}, not {kind}")
+    raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is on {t.device}, the current CUDA device is {device}")
+
+
+def _vector(t, n, kind, device, who, what):
+    """Address of `n` contiguous elements of type `kind` (a raw address, or None, is passed on)."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is kind and t.numel() >= n and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
+    if t.dtype is not kind:
+        raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is {t.dtype}, not {kind}")
+    if t.numel() < n or not t.is_contiguous():
+        raise MoeError(MOE_ERR_SHAPE, who, f"{what} is not {n} contiguous elements")
+    raise MoeError(MOE_ERR_UNSUPPORTED, who, f"{what} is on {t.device}, the current CUDA device is {device}")
+
+
+def _raw_stream(stream, device):
+    """As _stream, for a caller that has looked up the current device."""
+    if stream is None:
+        raw = _current_raw_stream
+        return raw(device) if raw else _stream(None)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def moe_permute(h, tokens, inv_perm, shape, rows, status_dev, stream=None):
@@ -477,8 +492,8 @@ def moe_permute(h, tokens, inv_perm, shape, rows, status_dev, stream=None):
     who, dev, R = "moe_permute", _device(), shape.T * shape.k_tot
     a, lda = _matrix(tokens, shape.T, shape.H, tokens.dtype, dev, who, "tokens")
     b, ldb = _matrix(rows, R, shape.H, tokens.dtype, dev, who, "rows")
-    _check(lib().moe_permute(h, a, lda, _vector(inv_perm, R, "torch.int32", dev, who, "inv_perm"), C.byref(shape), _row_type(tokens, who), b, ldb,
-                             _ptr(status_dev), _stream(stream)), who, h)
+    _check((_lib or lib()).moe_permute(h, a, lda, _vector(inv_perm, R, _i32, dev, who, "inv_perm"), C.byref(shape), _row_type(tokens.dtype, who), b, ldb,
+                             _ptr(status_dev), _raw_stream(stream, dev)), who, h)
 
 
 def moe_permute_grad(h, d_rows, inv_perm, shape, d_tokens, status_dev, stream=None):
@@ -486,8 +501,8 @@ def moe_permute_grad(h, d_rows, inv_perm, shape, d_tokens, status_dev, stream=No
     who, dev, R = "moe_permute_grad", _device(), shape.T * shape.k_tot
     a, lda = _matrix(d_rows, R, shape.H, d_rows.dtype, dev, who, "d_rows")
     b, ldb = _matrix(d_tokens, shape.T, shape.H, d_rows.dtype, dev, who, "d_tokens")
-    _check(lib().moe_permute_grad(h, a, lda, _vector(inv_perm, R, "torch.int32", dev, who, "inv_perm"), C.byref(shape), _row_type(d_rows, who), b, ldb,
-                                  _ptr(status_dev), _stream(stream)), who, h)
+    _check((_lib or lib()).moe_permute_grad(h, a, lda, _vector(inv_perm, R, _i32, dev, who, "inv_perm"), C.byref(shape), _row_type(d_rows.dtype, who), b, ldb,
+                                  _ptr(status_dev), _raw_stream(stream, dev)), who, h)
 
 
 def moe_unpermute(h, rows, inv_perm, topk_w, shape, out, status_dev, stream=None):
@@ -495,9 +510,9 @@ def moe_unpermute(h, rows, inv_perm, topk_w, shape, out, status_dev, stream=None
     who, dev, R = "moe_unpermute", _device(), shape.T * shape.k_tot
     a, lda = _matrix(rows, R, shape.H, rows.dtype, dev, who, "rows")
     b, ldb = _matrix(out, shape.T, shape.H, rows.dtype, dev, who, "out")
-    _check(lib().moe_unpermute(h, a, lda, _vector(inv_perm, R, "torch.int32", dev, who, "inv_perm"),
-                               _vector(topk_w, R, "torch.float32", dev, who, "topk_w"), C.byref(shape), _row_type(rows, who), b, ldb,
-                               _ptr(status_dev), _stream(stream)), who, h)
+    _check((_lib or lib()).moe_unpermute(h, a, lda, _vector(inv_perm, R, _i32, dev, who, "inv_perm"),
+                               _vector(topk_w, R, _f32, dev, who, "topk_w"), C.byref(shape), _row_type(rows.dtype, who), b, ldb,
+                               _ptr(status_dev), _raw_stream(stream, dev)), who, h)
 
 
 def moe_unpermute_grad(h, d_out, rows, inv_perm, topk_w, shape, d_rows, d_topk_w, status_dev, stream=None):
@@ -506,9 +521,9 @@ def moe_unpermute_grad(h, d_out, rows, inv_perm, topk_w, shape, d_rows, d_topk_w
     a, lda = _matrix(d_out, shape.T, shape.H, d_out.dtype, dev, who, "d_out")
     b, ldb = _matrix(rows, R, shape.H, d_out.dtype, dev, who, "rows")
     c, ldc = _matrix(d_rows, R, shape.H, d_out.dtype, dev, who, "d_rows")
-    _check(lib().moe_unpermute_grad(h, a, lda, b, ldb, _vector(inv_perm, R, "torch.int32", dev, who, "inv_perm"),
-                                    _vector(topk_w, R, "torch.float32", dev, who, "topk_w"), C.byref(shape), _row_type(d_out, who), c, ldc,
-                                    _vector(d_topk_w, R, "torch.float32", dev, who, "d_topk_w"), _ptr(status_dev), _stream(stream)), who, h)
+    _check((_lib or lib()).moe_unpermute_grad(h, a, lda, b, ldb, _vector(inv_perm, R, _i32, dev, who, "inv_perm"),
+                                    _vector(topk_w, R, _f32, dev, who, "topk_w"), C.byref(shape), _row_type(d_out.dtype, who), c, ldc,
+                                    _vector(d_topk_w, R, _f32, dev, who, "d_topk_w"), _ptr(status_dev), _raw_stream(stream, dev)), who, h)
 
 
 def moe_gated_act(h, gate_up, act, codes=None, scales=None, stream=None):
@@ -518,8 +533,8 @@ def moe_gated_act(h, gate_up, act, codes=None, scales=None, stream=None):
     rows, I = gate_up.shape[0], gate_up.shape[-1] // 2
     a, lda = _matrix(gate_up, rows, 2 * I, gate_up.dtype, dev, who, "gate_up")
     b, ldb = _matrix(act, rows, I, gate_up.dtype, dev, who, "act")
-    _check(lib().moe_gated_act(h, a, lda, rows, I, _row_type(gate_up, who), b, ldb, _vector(codes, rows * 2 * I, "torch.uint8", dev, who, "codes"),
-                               _vector(scales, rows * 2 * ((I + 31) // 32), "torch.uint8", dev, who, "scales"), _stream(stream)), who, h)
+    _check((_lib or lib()).moe_gated_act(h, a, lda, rows, I, _row_type(gate_up.dtype, who), b, ldb, _vector(codes, rows * 2 * I, _u8, dev, who, "codes"),
+                               _vector(scales, rows * 2 * ((I + 31) // 32), _u8, dev, who, "scales"), _raw_stream(stream, dev)), who, h)
 
 
 def moe_gated_act_grad(h, d_act, codes, scales, d_gate_up, act=None, stream=None):
@@ -529,22 +544,23 @@ def moe_gated_act_grad(h, d_act, codes, scales, d_gate_up, act=None, stream=None
     a, lda = _matrix(d_act, rows, I, d_act.dtype, dev, who, "d_act")
     b, ldb = _matrix(d_gate_up, rows, 2 * I, d_act.dtype, dev, who, "d_gate_up")
     c, ldc = _matrix(act, rows, I, d_act.dtype, dev, who, "act") if act is not None else (None, 0)
-    _check(lib().moe_gated_act_grad(h, a, lda, _vector(codes, rows * 2 * I, "torch.uint8", dev, who, "codes"),
-                                    _vector(scales, rows * 2 * ((I + 31) // 32), "torch.uint8", dev, who, "scales"), rows, I, _row_type(d_act, who),
-                                    b, ldb, c, ldc, _stream(stream)), who, h)
+    _check((_lib or lib()).moe_gated_act_grad(h, a, lda, _vector(codes, rows * 2 * I, _u8, dev, who, "codes"),
+                                    _vector(scales, rows * 2 * ((I + 31) // 32), _u8, dev, who, "scales"), rows, I, _row_type(d_act.dtype, who),
+                                    b, ldb, c, ldc, _raw_stream(stream, dev)), who, h)
 
 
 def moe_mxfp4_scale_bytes(rows: int, K: int, groups: int) -> int:
     b = C.c_size_t()
-    _check(lib().moe_mxfp4_scale_bytes(rows, K, groups, C.byref(b)), "moe_mxfp4_scale_bytes")
+    _check((_lib or lib()).moe_mxfp4_scale_bytes(rows, K, groups, C.byref(b)), "moe_mxfp4_scale_bytes")
     return b.value
 
 
 def _mxfp4_operand(codes, scales, groups, dev, who, what=""):
     """(address of the codes, address of the exponents, rows, K); codes uint8 [..., K / 2] contiguous."""
-    rows, K = codes.numel() // max(1, codes.shape[-1]), 2 * codes.shape[-1]
-    need = moe_mxfp4_scale_bytes(rows, K, groups)
-    return (_vector(codes, rows * K // 2, "torch.uint8", dev, who, what + "codes"), _vector(scales, need, "torch.uint8", dev, who, what + "scales"), rows, K)
+    half, n = codes.shape[-1], codes.numel()
+    rows, K = n // max(1, half), 2 * half
+    need = (rows // 128 + groups) * ((K + 127) // 128) * 512            # moe_mxfp4_scale_bytes, whose checks the call repeats
+    return (_vector(codes, n, _u8, dev, who, what + "codes"), _vector(scales, need, _u8, dev, who, what + "scales"), rows, K)
 
 
 def moe_mxfp4_quantize(h, src, codes, scales, groups, status_dev, offsets=None, inv_perm=None, stream=None):
@@ -556,8 +572,8 @@ def moe_mxfp4_quantize(h, src, codes, scales, groups, status_dev, offsets=None, 
     if inv_perm is not None and inv_perm.numel() != rows:
         raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm names {inv_perm.numel()} rows, codes have {rows}")
     a, lda = _matrix(src, rows // max(1, copies), K, src.dtype, dev, who, "src")
-    _check(lib().moe_mxfp4_quantize(h, a, lda, _row_type(src, who), rows, K, groups, _vector(offsets, groups + 1, "torch.int32", dev, who, "offsets"),
-                                    _vector(inv_perm, rows, "torch.int32", dev, who, "inv_perm"), copies, c, sc, _ptr(status_dev), _stream(stream)), who, h)
+    _check((_lib or lib()).moe_mxfp4_quantize(h, a, lda, _row_type(src.dtype, who), rows, K, groups, _vector(offsets, groups + 1, _i32, dev, who, "offsets"),
+                                    _vector(inv_perm, rows, _i32, dev, who, "inv_perm"), copies, c, sc, _ptr(status_dev), _raw_stream(stream, dev)), who, h)
 
 
 def moe_mxfp4_dequantize(h, codes, scales, groups, out, status_dev, offsets=None, stream=None):
@@ -565,8 +581,8 @@ def moe_mxfp4_dequantize(h, codes, scales, groups, out, status_dev, offsets=None
     who, dev = "moe_mxfp4_dequantize", _device()
     c, sc, rows, K = _mxfp4_operand(codes, scales, groups, dev, who)
     a, lda = _matrix(out, rows, K, out.dtype, dev, who, "out")
-    _check(lib().moe_mxfp4_dequantize(h, c, sc, rows, K, groups, _vector(offsets, groups + 1, "torch.int32", dev, who, "offsets"), _row_type(out, who),
-                                      a, lda, _ptr(status_dev), _stream(stream)), who, h)
+    _check((_lib or lib()).moe_mxfp4_dequantize(h, c, sc, rows, K, groups, _vector(offsets, groups + 1, _i32, dev, who, "offsets"), _row_type(out.dtype, who),
+                                      a, lda, _ptr(status_dev), _raw_stream(stream, dev)), who, h)
 
 
 def moe_mxfp4_gemm(h, x_codes, x_scales, w_codes, w_scales, offsets, out, status_dev, stream=None):
@@ -580,8 +596,8 @@ def moe_mxfp4_gemm(h, x_codes, x_scales, w_codes, w_scales, offsets, out, status
     if K != Kw:
         raise MoeError(MOE_ERR_SHAPE, who, f"x has {K} columns, w {Kw}")
     a, lda = _matrix(out, rows, N, out.dtype, dev, who, "out")
-    _check(lib().moe_mxfp4_gemm(h, x, xs, w, ws, _vector(offsets, E + 1, "torch.int32", dev, who, "offsets"), rows, E, N, K, _row_type(out, who), a, lda,
-                                _ptr(status_dev), _stream(stream)), who, h)
+    _check((_lib or lib()).moe_mxfp4_gemm(h, x, xs, w, ws, _vector(offsets, E + 1, _i32, dev, who, "offsets"), rows, E, N, K, _row_type(out.dtype, who), a, lda,
+                                _ptr(status_dev), _raw_stream(stream, dev)), who, h)
 
 
 # ----------------------------------------------------------------------------- device memory plumbing

@@ -41,9 +41,9 @@ Divisor divisor_of(int32_t d)
     return r;
 }
 
-// 128B swizzle, every element of a box; false, with a message in the handle, when it cannot be encoded
+// Every element of a box; false, with a message in the handle, when it cannot be encoded
 static bool encode_map(moe_handle *h, CUtensorMap *map, CUtensorMapDataType type, const void *ptr, int rank, const cuuint64_t *dims,
-                       const cuuint64_t *strides, const cuuint32_t *box, const char *name)
+                       const cuuint64_t *strides, const cuuint32_t *box, const char *name, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B)
 {
     typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                       const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -51,7 +51,7 @@ static bool encode_map(moe_handle *h, CUtensorMap *map, CUtensorMapDataType type
     const cuuint32_t es[5] = {1, 1, 1, 1, 1};
     const CUresult cr = reinterpret_cast<EncodeTiledFn>(h->encode_tiled)(
         map, type, (cuuint32_t)rank, const_cast<void *>(ptr), dims, strides, box, es,
-        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (cr == CUDA_SUCCESS) return true;
     snprintf(h->err, sizeof h->err, "cuTensorMapEncodeTiled(%s) failed: %d", name, (int)cr);
     return false;
@@ -88,6 +88,15 @@ bool code_map(moe_handle *h, CUtensorMap *map, const void *ptr, int32_t planes, 
     const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)row_bytes * (cuuint64_t)rows};
     const cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1};
     return encode_map(h, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, ptr, planes ? 3 : 2, dims, strides, box, name);
+}
+
+bool scale_map(moe_handle *h, CUtensorMap *map, const void *ptr, int64_t row_blocks, int32_t col_blocks, const char *name)
+{
+    // a block's 512 bytes as 128 words: a box has at most 256 elements a side
+    const cuuint64_t dims[3] = {128, (cuuint64_t)col_blocks, (cuuint64_t)row_blocks};
+    const cuuint64_t strides[2] = {512, 512 * (cuuint64_t)col_blocks};
+    const cuuint32_t box[3] = {128, 2, 2};
+    return encode_map(h, map, CU_TENSOR_MAP_DATA_TYPE_UINT32, ptr, 3, dims, strides, box, name, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 const CUtensorMap *gate_up_map(moe_handle *h, const void *ptr, int32_t experts, int32_t inter, int32_t cols, int32_t box_inter, const char *name)

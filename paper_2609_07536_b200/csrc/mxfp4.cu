@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
 // Tile: 128 columns of the output x up to 192 rows.  TMEM holds two accumulators of 192 columns and, for every operand stage, 24
 // columns of exponents (128 rows of weights: 4 per 128 columns of K; 256 rows of x: 8); that is 504 of its 512 columns, and why a
 // tile has 192 rows and not 256.  A stage is 256 columns of K: 128 bytes of codes a row, a swizzle row.
-//   warp 0      TMA producer (one thread): codes of weights and rows, and their exponents as they lie;
+//   warps 0, 2  loaders (one thread each): codes of the weights, of the rows, and their exponents as they lie;
 //   warp 1      copies the exponents to TMEM (tcgen05.cp, each of the four lane quarters gets them) and issues
 //               tcgen05.mma.kind::mxf4.block_scale (K = 64, two exponents a row); both are issued by one lane of the converged
 //               warp and run in order;
@@ -179,7 +179,6 @@ constexpr int kPrThreads = 384, kPrEpiWarps = 8;
 constexpr int kPrN = 128;                                   // output columns of a tile (M of the MMA)
 constexpr int kPrRows = 192;                                // rows of a tile (N of the MMA)
 constexpr int kPrK = 256, kPrStepK = 64;                    // columns of K of a stage, of an MMA
-constexpr int kPrBoxRows = 64;                              // rows that one copy of x brings
 constexpr int kPrStages = 5;
 constexpr int kPrWBytes = kPrN * kPrK / 2, kPrXBytes = kPrRows * kPrK / 2;
 constexpr int kPrWScaleBytes = 2 * kMxTileBytes, kPrXScaleBytes = 4 * kMxTileBytes;      // x: row block 0 of both 128s of K, then row block 1
@@ -191,9 +190,10 @@ static_assert(2 * kPrRows + kPrStages * kPrScaleCols <= kPrTmemCols, "accumulato
 static_assert(kPrStageBytes % 1024 == 0, "stages are 1024-byte aligned");
 
 struct alignas(64) ProductParams {
-    CUtensorMap tmW;   // codes [E][N][K / 2]   box 128 bytes x 128 rows, 128B swizzle
-    CUtensorMap tmX;   // codes [R][K / 2]      box 128 bytes x 64 rows
-    const uint8_t *w_scales, *x_scales;
+    CUtensorMap tmW;               // codes [E][N][K / 2]   box 128 bytes x 128 rows, 128B swizzle
+    CUtensorMap tmX[3];            // codes [R][K / 2]      box 128 bytes x 192, 64, 16 rows
+    CUtensorMap tmXs;              // exponents of x [row blocks][KQ][512 bytes]   box 2 row blocks x 2 x 512 bytes
+    const uint8_t *w_scales;
     const int32_t *offsets;        // [E + 1]
     void *out;
     long long ld_out;              // elements
@@ -213,6 +213,7 @@ struct ProductControl {
 __device__ __forceinline__ bool pr_wait(uint32_t bar, uint32_t parity, ProductControl *ctl, unsigned long long deadline, uint32_t *status,
                                         uint32_t detail, uint32_t where)
 {
+    if (mbar_test_wait(bar, parity)) return true;
     uint32_t spins = 0;
     while (!mbar_try_wait(bar, parity)) {
         if ((++spins & 63u) == 0u) {
@@ -227,48 +228,94 @@ __device__ __forceinline__ bool pr_wait(uint32_t bar, uint32_t parity, ProductCo
     return true;
 }
 
+// The tiles of a CTA: row tile outer, column tile inner, every gridDim.x-th one.  The expert is found by a vote of the warp for the first
+// tile and by steps from there on (found by bisection for every tile, and the addresses worked out from nothing, a tile's start cost
+// 1500 cycles in every role, of 9000 that a tile of 2048 columns took).
 struct ProductTile {
     int e, row0, valid, local, n0;     // local: first row inside the expert
 };
-__device__ __forceinline__ ProductTile pr_tile(int g, const ProductParams &P, const ProductControl *ctl)
-{
-    const int mu = quotient(P.by_NT, g);
-    int lo = 0, hi = P.E - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (ctl->tiles[mid] <= mu) lo = mid;
-        else hi = mid - 1;
+struct ProductWalk {
+    int g, e;
+    // (the whole warp)
+    __device__ __forceinline__ ProductWalk(const ProductParams &P, const ProductControl *ctl) : g((int)blockIdx.x), e(-1)
+    {
+        const int mu = quotient(P.by_NT, g), lane = threadIdx.x & 31;
+        for (int i = 0; i < P.E; i += 32) e += __popc(__ballot_sync(0xffffffffu, i + lane < P.E && ctl->tiles[i + lane] <= mu));
     }
-    ProductTile t;
-    t.e = lo;
-    t.local = (mu - ctl->tiles[lo]) * kPrRows;
-    t.row0 = ctl->first[lo] + t.local;
-    t.valid = min(kPrRows, ctl->first[lo + 1] - t.row0);
-    t.n0 = (g - mu * P.NT) * kPrN;
-    return t;
-}
+    __device__ __forceinline__ void next() { g += (int)gridDim.x; }
+    __device__ __forceinline__ ProductTile tile(const ProductParams &P, const ProductControl *ctl)
+    {
+        const int mu = quotient(P.by_NT, g);
+        while (ctl->tiles[e + 1] <= mu) ++e;       // (g is a tile that there is)
+        ProductTile t;
+        t.e = e;
+        t.local = (mu - ctl->tiles[e]) * kPrRows;
+        t.row0 = ctl->first[e] + t.local;
+        t.valid = min(kPrRows, ctl->first[e + 1] - t.row0);
+        t.n0 = (g - mu * P.NT) * kPrN;
+        return t;
+    }
+};
 
 // Instruction descriptor, kind::mxf4: e2m1 operands, K-major, M = 128, exponents of type ue8m0, exponent pair `half` of the column's four bytes
 __device__ __forceinline__ uint32_t mxf4_idesc(uint32_t n, uint32_t half)
 {
     return (2u * half << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((uint32_t)(kPrN >> 4) << 24) | (2u * half << 29);
 }
-__device__ __forceinline__ void tc_mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t a_scale, uint32_t b_scale,
-                                            uint32_t accumulate)
+// Exponents, shared memory -> TMEM: 512 contiguous bytes are 32 rows of 16, which become 32 lanes x 4 columns in each of the four lane
+// quarters.  Descriptor: no swizzle, eights of rows 128 bytes apart (stride offset), version 1.
+constexpr uint32_t kScaleDescHi = (128u >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t scale_desc_lo(uint32_t smem) { return ((smem & 0x3FFFFu) >> 4) | (1u << 16); }
+// One stage of operands in one statement: the exponents' copies (`two`: two row blocks of x), `steps` MMAs and the commit that hands the
+// stage back.  All of them are issued by one thread and run in order.
+__device__ __forceinline__ void tc_kblock_mxf4(uint32_t d_tmem, uint32_t w_lo, uint32_t x_lo, uint32_t ws_lo, uint32_t xs_lo, uint32_t sw, uint32_t sx,
+                                               uint32_t shift, uint32_t two, uint32_t idesc0, uint32_t idesc1, uint32_t accumulate, uint32_t steps,
+                                               uint32_t empty_bar)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+        "{\n\t.reg .pred p, q, t, t1, s1, s2, s3;\n\t.reg .b64 da, db;\n\t.reg .b32 al, bl, sa, sb;\n\t"
+        "setp.ne.b32 p, %11, 0;\n\t"
+        "setp.eq.b32 q, %11, %11;\n\t"
+        "setp.ne.b32 t, %8, 0;\n\t"
+        "setp.gt.u32 s1, %12, 1;\n\t"
+        "setp.gt.u32 s2, %12, 2;\n\t"
+        "setp.gt.u32 s3, %12, 3;\n\t"
+        "and.pred t1, t, s2;\n\t"
+        // exponents of the first 128 columns, then of the second
+        "mov.b64 da, {%3, %15};\n\t"
+        "tcgen05.cp.cta_group::1.32x128b.warpx4 [%5], da;\n\t"
+        "mov.b64 da, {%4, %15};\n\t"
+        "tcgen05.cp.cta_group::1.32x128b.warpx4 [%6], da;\n\t"
+        "add.u32 al, %4, 64;\n\tadd.u32 sa, %6, 4;\n\t"
+        "mov.b64 da, {al, %15};\n\t"
+        "@t tcgen05.cp.cta_group::1.32x128b.warpx4 [sa], da;\n\t"
+        "add.u32 al, %3, 32;\n\tadd.u32 sa, %5, 4;\n\t"
+        "mov.b64 da, {al, %15};\n\t"
+        "@s2 tcgen05.cp.cta_group::1.32x128b.warpx4 [sa], da;\n\t"
+        "add.u32 al, %4, 32;\n\tadd.u32 sa, %6, 8;\n\t"
+        "mov.b64 da, {al, %15};\n\t"
+        "@s2 tcgen05.cp.cta_group::1.32x128b.warpx4 [sa], da;\n\t"
+        "add.u32 al, %4, 96;\n\tadd.u32 sa, %6, 12;\n\t"
+        "mov.b64 da, {al, %15};\n\t"
+        "@t1 tcgen05.cp.cta_group::1.32x128b.warpx4 [sa], da;\n\t"
+        // products: 64 columns are 32 bytes further along the swizzle row
+        "add.u32 sb, %6, %7;\n\t"
+        "mov.b64 da, {%1, %14};\n\tmov.b64 db, {%2, %14};\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [%5], [sb], p;\n\t"
+        "add.u32 al, %1, 2;\n\tadd.u32 bl, %2, 2;\n\t"
+        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t"
+        "@s1 tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [%5], [sb], q;\n\t"
+        "add.u32 sa, %5, 4;\n\tadd.u32 sb, sb, 8;\n\t"
+        "add.u32 al, %1, 4;\n\tadd.u32 bl, %2, 4;\n\t"
+        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t"
+        "@s2 tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [sa], [sb], q;\n\t"
+        "add.u32 al, %1, 6;\n\tadd.u32 bl, %2, 6;\n\t"
+        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t"
+        "@s3 tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [sa], [sb], q;\n\t"
+        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%13];\n\t}"
+        ::"r"(d_tmem), "r"(w_lo), "r"(x_lo), "r"(ws_lo), "r"(xs_lo), "r"(sw), "r"(sx), "r"(shift), "r"(two), "r"(idesc0), "r"(idesc1), "r"(accumulate),
+        "r"(steps), "r"(empty_bar), "r"(kSmemDescHi), "r"(kScaleDescHi)
         : "memory");
-}
-// 32 rows of 16 bytes of shared memory (512 contiguous bytes) -> 32 lanes x 4 columns of TMEM, in each of the four lane quarters
-__device__ __forceinline__ void tc_cp_scales(uint32_t d_tmem, uint32_t smem)
-{
-    // no swizzle; eights of rows 128 bytes apart (stride offset); version 1
-    const uint64_t desc = ((uint64_t)((128u >> 4) | (1u << 14)) << 32) | ((smem & 0x3FFFFu) >> 4) | (1u << 16);
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(d_tmem), "l"(desc) : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
@@ -310,6 +357,17 @@ __device__ __forceinline__ void store_piece(const uint32_t (&lo)[16], const uint
     }
 }
 
+// A loader's wind-down: the copies already issued land before shared memory is released
+__device__ __forceinline__ void pr_drain(ProductControl *ctl, uint32_t armed, int stage, uint32_t phase)
+{
+    const unsigned long long drain = globaltimer_ns() + 2000000ull;
+    for (int i = 0; i < kPrStages; ++i) {
+        if (!(armed & (1u << i))) continue;
+        const uint32_t par = i < stage ? phase : (phase ^ 1u);
+        while (!mbar_try_wait(smem_u32(&ctl->full[i]), par) && globaltimer_ns() < drain) {}
+    }
+}
+
 template <class E>
 __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __grid_constant__ ProductParams P)
 {
@@ -319,7 +377,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kPrStages; ++i) {
-            mbar_init(smem_u32(&ctl->full[i]), 1);
+            mbar_init(smem_u32(&ctl->full[i]), 2);            // the two loaders
             mbar_init(smem_u32(&ctl->empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -331,16 +389,20 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         prefetch_tensormap(&P.tmW);
-        prefetch_tensormap(&P.tmX);
+        prefetch_tensormap(&P.tmX[0]);
+        prefetch_tensormap(&P.tmXs);
     }
     if (warp == 1) tmem_alloc(smem_u32(&ctl->tmem_base), kPrTmemCols);
     grid_dependency_wait();
-    if (warp == 2) {
+    for (int e = threadIdx.x; e <= P.E; e += kPrThreads) ctl->first[e] = ld_chained(P.offsets + e);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 3) {
         // where the experts' rows begin and how many row tiles lie before them; what is out of range is reported and has no rows
         int tiles = 0, before = 0;
         for (int e0 = 0; e0 <= P.E; e0 += 32) {
-            const int e = e0 + lane;
-            const int raw = ld_chained(P.offsets + min(e, P.E));
+            const int e = e0 + lane, raw = ctl->first[min(e, P.E)];
             int o = min(max(raw, before), P.R);
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {                     // running maximum: offsets never go back
@@ -365,84 +427,92 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             tiles += __shfl_sync(0xffffffffu, t, 31);
         }
     }
-    tc_fence_before();
     __syncthreads();
-    tc_fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
-    const int total = ctl->tiles[P.E] * P.NT, stride = (int)gridDim.x;
+    const int total = ctl->tiles[P.E] * P.NT;
     const unsigned long long deadline = globaltimer_ns() + P.wait_ns;
+    ProductWalk walk(P, ctl);
 
+    // Two loaders, one thread each: a copy's issue takes its thread about 100 cycles whatever it copies, and with one thread for the seven
+    // copies that a stage then took (x in boxes of 64 rows, exponents of two row blocks) the issue alone was 720 of a stage's 1100 cycles.
     if (warp == 0) {
         if (lane == 0) {
             int stage = 0;
             uint32_t phase = 0, armed = 0;
             bool ok = true;
-            for (int g = (int)blockIdx.x; g < total && ok; g += stride) {
-                const ProductTile t = pr_tile(g, P, ctl);
-                const int boxes = (t.valid + kPrBoxRows - 1) / kPrBoxRows;
-                const int shift = t.local & (kMxTile - 1);                     // 0 or 64: first row inside its exponent block
-                const int xblocks = shift + t.valid > kMxTile ? 2 : 1;
-                const long long row_bytes = (long long)P.KQ * kMxTileBytes;
-                // the offset that the quantisation used: the expert's first row (t.row0 - t.local)
-                const uint8_t *xs = P.x_scales + ((long long)((t.row0 - t.local) / kMxTile) + t.e + t.local / kMxTile) * row_bytes;
+            const long long row_bytes = (long long)P.KQ * kMxTileBytes;
+            for (; walk.g < total && ok; walk.next()) {
+                const ProductTile t = walk.tile(P, ctl);
                 const uint8_t *ws = P.w_scales + ((long long)t.e * P.N / kMxTile + t.e + t.n0 / kMxTile) * row_bytes;
-                for (int kb = 0; kb < P.num_kb; ++kb) {
-                    ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)g, 70u);
+                for (int kb = 0; kb < P.num_kb; ++kb, ws += 2 * kMxTileBytes) {
+                    ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 70u);
                     if (!ok) break;
-                    const uint32_t bar = smem_u32(&ctl->full[stage]), w_dst = smem_u32(ring + stage * kPrStageBytes);
-                    const uint32_t x_dst = w_dst + kPrWBytes, ws_dst = x_dst + kPrXBytes, xs_dst = ws_dst + kPrWScaleBytes;
-                    const uint32_t sb = (uint32_t)min(2, P.KQ - 2 * kb) * kMxTileBytes;      // exponents of a row block
-                    mbar_arrive_expect_tx(bar, kPrWBytes + (uint32_t)boxes * (kPrBoxRows * kPrK / 2) + sb * (1u + (uint32_t)xblocks));
-                    tma_load_3d(w_dst, &P.tmW, bar, kb * (kPrK / 2), t.n0, t.e);
-                    for (int b = 0; b < boxes; ++b)
-                        tma_load_2d(x_dst + (uint32_t)b * (kPrBoxRows * kPrK / 2), &P.tmX, bar, kb * (kPrK / 2), t.row0 + b * kPrBoxRows);
-                    bulk_load(ws_dst, ws + kb * (2 * kMxTileBytes), sb, bar);
-                    for (int b = 0; b < xblocks; ++b)
-                        bulk_load(xs_dst + (uint32_t)b * (2 * kMxTileBytes), xs + b * row_bytes + kb * (2 * kMxTileBytes), sb, bar);
+                    const uint32_t bar = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * kPrStageBytes);
+                    const uint32_t sb = (uint32_t)min(2, P.KQ - 2 * kb) * kMxTileBytes;      // exponents that there are
+                    mbar_arrive_expect_tx(bar, kPrWBytes + sb);
+                    tma_load_3d(dst, &P.tmW, bar, kb * (kPrK / 2), t.n0, t.e);
+                    bulk_load(dst + kPrWBytes + kPrXBytes, ws, sb, bar);
                     armed |= 1u << stage;
                     if (++stage == kPrStages) { stage = 0; phase ^= 1u; }
                 }
             }
-            if (!ok) {
-                // wind-down: let the copies already issued land before shared memory is released
-                const unsigned long long drain = globaltimer_ns() + 2000000ull;
-                for (int i = 0; i < kPrStages; ++i) {
-                    if (!(armed & (1u << i))) continue;
-                    const uint32_t par = i < stage ? phase : (phase ^ 1u);
-                    while (!mbar_try_wait(smem_u32(&ctl->full[i]), par) && globaltimer_ns() < drain) {}
+            if (!ok) pr_drain(ctl, armed, stage, phase);
+        }
+        __syncwarp();
+    } else if (warp == 2) {
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0, armed = 0;
+            bool ok = true;
+            for (; walk.g < total && ok; walk.next()) {
+                const ProductTile t = walk.tile(P, ctl);
+                // 192 rows, or 64s of them, or 16: the rows behind the tile's own are read for nothing
+                const int which = t.valid > 2 * 64 ? 0 : t.valid > 16 ? 1 : 2, boxes = which == 1 && t.valid > 64 ? 2 : 1;
+                const uint32_t box_bytes = (which == 0 ? kPrRows : which == 1 ? 64u : 16u) * (kPrK / 2);
+                const CUtensorMap *map = &P.tmX[which];
+                // the row block that the quantisation put the tile's first row into: by the expert's first row (row0 - local)
+                const int block = (t.row0 - t.local) / kMxTile + t.e + t.local / kMxTile;
+                for (int kb = 0; kb < P.num_kb; ++kb) {
+                    ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 74u);
+                    if (!ok) break;
+                    const uint32_t bar = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * kPrStageBytes) + kPrWBytes;
+                    mbar_arrive_expect_tx(bar, (uint32_t)boxes * box_bytes + kPrXScaleBytes);
+                    tma_load_2d(dst, map, bar, kb * (kPrK / 2), t.row0);
+                    if (boxes == 2) tma_load_2d(dst + box_bytes, map, bar, kb * (kPrK / 2), t.row0 + 64);
+                    tma_load_3d(dst + kPrXBytes + kPrWScaleBytes, &P.tmXs, bar, 0, 2 * kb, block);
+                    armed |= 1u << stage;
+                    if (++stage == kPrStages) { stage = 0; phase ^= 1u; }
                 }
             }
+            if (!ok) pr_drain(ctl, armed, stage, phase);
         }
         __syncwarp();
     } else if (warp == 1) {
+        // the whole warp runs the loop, converged, and one elected lane issues: warp-uniform operands (see the other products)
         int stage = 0, it = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int g = (int)blockIdx.x; g < total && ok; g += stride, ++it) {
-            const ProductTile t = pr_tile(g, P, ctl);
-            const int a = it & 1, shift = t.local & (kMxTile - 1), xblocks = shift + t.valid > kMxTile ? 2 : 1;
-            const uint32_t n = (uint32_t)((t.valid + 15) & ~15), idesc0 = mxf4_idesc(n, 0u), idesc1 = mxf4_idesc(n, 1u);
-            ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), ((uint32_t)(it >> 1) & 1u) ^ 1u, ctl, deadline, P.status, (uint32_t)g, 71u));
+        const uint32_t ring0 = smem_u32(ring), lo0 = smem_desc_lo(ring0), sc0 = scale_desc_lo(ring0), full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
+        for (; walk.g < total && ok; walk.next(), ++it) {
+            const ProductTile t = walk.tile(P, ctl);
+            const int a = it & 1;
+            const uint32_t shift = (uint32_t)(t.local & (kMxTile - 1)) >> 5;                 // 0 or 2 columns: first row inside its row block
+            const uint32_t n = __reduce_max_sync(0xffffffffu, (uint32_t)((t.valid + 15) & ~15)), two = 32u * shift + n > (uint32_t)kMxTile ? 1u : 0u;
+            const uint32_t idesc0 = mxf4_idesc(n, 0u), idesc1 = mxf4_idesc(n, 1u);
+            ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), ((uint32_t)(it >> 1) & 1u) ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 71u));
             if (!ok) break;
             tc_fence_after();
             const uint32_t d_tmem = tmem_base + (uint32_t)(a * kPrRows);
             for (int kb = 0; kb < P.num_kb; ++kb) {
-                ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->full[stage]), phase, ctl, deadline, P.status, (uint32_t)g, 72u));
+                ok = __all_sync(0xffffffffu, pr_wait(full0 + 8u * stage, phase, ctl, deadline, P.status, (uint32_t)walk.g, 72u));
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one_sync()) {
-                    const uint32_t w = smem_u32(ring + stage * kPrStageBytes), x = w + kPrWBytes, ws = x + kPrXBytes, xs = ws + kPrWScaleBytes;
-                    const uint32_t sw = tmem_base + (uint32_t)(2 * kPrRows + stage * kPrScaleCols), sx = sw + 8u;
-                    const int steps = kb == P.num_kb - 1 ? P.last_steps : kPrK / kPrStepK, quarters = (steps + 1) >> 1;
-                    for (int q = 0; q < quarters; ++q) {
-                        tc_cp_scales(sw + 4u * q, ws + q * kMxTileBytes);
-                        for (int b = 0; b < xblocks; ++b) tc_cp_scales(sx + 8u * q + 4u * b, xs + (2 * b + q) * kMxTileBytes);
-                    }
-                    const uint64_t wd = ((uint64_t)kSmemDescHi << 32) | smem_desc_lo(w), xd = ((uint64_t)kSmemDescHi << 32) | smem_desc_lo(x);
-                    for (int k = 0; k < steps; ++k)
-                        tc_mma_mxf4(d_tmem, wd + (uint64_t)(2 * k), xd + (uint64_t)(2 * k), k & 1 ? idesc1 : idesc0, sw + 4u * (k >> 1),
-                                    sx + 8u * (k >> 1) + (uint32_t)(shift >> 5), (k > 0 || kb > 0) ? 1u : 0u);
-                    tc_commit(smem_u32(&ctl->empty[stage]));
+                    constexpr uint32_t kX = kPrWBytes >> 4, kWs = (kPrWBytes + kPrXBytes) >> 4, kXs = kWs + (kPrWScaleBytes >> 4);
+                    const uint32_t w_lo = lo0 + (uint32_t)(stage * (kPrStageBytes >> 4)), s_lo = sc0 + (uint32_t)(stage * (kPrStageBytes >> 4));
+                    const uint32_t sw = tmem_base + (uint32_t)(2 * kPrRows + stage * kPrScaleCols);
+                    tc_kblock_mxf4(d_tmem, w_lo, w_lo + kX, s_lo + kWs, s_lo + kXs, sw, sw + 8u, shift, two, idesc0, idesc1, kb > 0 ? 1u : 0u,
+                                   kb == P.num_kb - 1 ? (uint32_t)P.last_steps : 4u, empty0 + 8u * stage);
                     if (kb == P.num_kb - 1) tc_commit(smem_u32(&ctl->tmem_full[a]));
                 }
                 __syncwarp();
@@ -460,11 +530,11 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     } else if (warp >= 4) {
         const int q4 = warp & 3, grp = (warp - 4) >> 2;
         int it = 0;
-        for (int g = (int)blockIdx.x; g < total; g += stride, ++it) {
-            const ProductTile t = pr_tile(g, P, ctl);
+        for (; walk.g < total; walk.next(), ++it) {
+            const ProductTile t = walk.tile(P, ctl);
             const int a = it & 1, pieces = (t.valid + 31) >> 5, col = t.n0 + q4 * 32, cols = P.N - col;
             uint32_t ok = 1u;
-            if (lane == 0) ok = pr_wait(smem_u32(&ctl->tmem_full[a]), (uint32_t)(it >> 1) & 1u, ctl, deadline, P.status, (uint32_t)g, 73u) ? 1u : 0u;
+            if (lane == 0) ok = pr_wait(smem_u32(&ctl->tmem_full[a]), (uint32_t)(it >> 1) & 1u, ctl, deadline, P.status, (uint32_t)walk.g, 73u) ? 1u : 0u;
             if (!__shfl_sync(0xffffffffu, ok, 0)) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(a * kPrRows);
@@ -607,7 +677,6 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     ProductParams p;
     memset(&p, 0, sizeof p);
     p.w_scales = static_cast<const uint8_t *>(w_scales);
-    p.x_scales = static_cast<const uint8_t *>(x_scales);
     p.offsets = offsets;
     p.out = out;
     p.ld_out = ld_out;
@@ -623,7 +692,9 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     p.by_NT = divisor_of(p.NT);
     const int64_t used = rows < E_tot ? rows : E_tot, tiles = ((rows - used) / kPrRows + used) * p.NT;      // at most
     if (tiles >= (int64_t)1 << 31) return MOE_ERR_SHAPE;
-    if (!code_map(h, &p.tmW, w_codes, E_tot, N, K / 2, kPrN, "w_codes") || !code_map(h, &p.tmX, x_codes, 0, rows, K / 2, kPrBoxRows, "x_codes"))
+    if (!code_map(h, &p.tmW, w_codes, E_tot, N, K / 2, kPrN, "w_codes") || !code_map(h, &p.tmX[0], x_codes, 0, rows, K / 2, kPrRows, "x_codes") ||
+        !code_map(h, &p.tmX[1], x_codes, 0, rows, K / 2, 64, "x_codes") || !code_map(h, &p.tmX[2], x_codes, 0, rows, K / 2, 16, "x_codes") ||
+        !scale_map(h, &p.tmXs, x_scales, scale_blocks(rows, E_tot), p.KQ, "x_scales"))
         return MOE_ERR_CUDA;
     const unsigned grid = (unsigned)(tiles < h->G ? tiles : h->G);
     const cudaError_t err = launch_chained(dtype == MOE_BF16 ? mxfp4_product_kernel<__nv_bfloat16> : mxfp4_product_kernel<__half>, grid, kPrThreads, kPrSmem,
