@@ -90,12 +90,12 @@ bool code_map(moe_handle *h, CUtensorMap *map, const void *ptr, int32_t planes, 
     return encode_map(h, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, ptr, planes ? 3 : 2, dims, strides, box, name);
 }
 
-bool scale_map(moe_handle *h, CUtensorMap *map, const void *ptr, int64_t row_blocks, int32_t col_blocks, const char *name)
+bool scale_map(moe_handle *h, CUtensorMap *map, const void *ptr, int64_t row_blocks, int32_t col_blocks, int32_t box_blocks, const char *name)
 {
     // a block's 512 bytes as 128 words: a box has at most 256 elements a side
     const cuuint64_t dims[3] = {128, (cuuint64_t)col_blocks, (cuuint64_t)row_blocks};
     const cuuint64_t strides[2] = {512, 512 * (cuuint64_t)col_blocks};
-    const cuuint32_t box[3] = {128, 2, 2};
+    const cuuint32_t box[3] = {128, 2, (cuuint32_t)box_blocks};
     return encode_map(h, map, CU_TENSOR_MAP_DATA_TYPE_UINT32, ptr, 3, dims, strides, box, name, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 

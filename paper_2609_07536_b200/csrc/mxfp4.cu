@@ -192,8 +192,7 @@ static_assert(kPrStageBytes % 1024 == 0, "stages are 1024-byte aligned");
 struct alignas(64) ProductParams {
     CUtensorMap tmW;               // codes [E][N][K / 2]   box 128 bytes x 128 rows, 128B swizzle
     CUtensorMap tmX[3];            // codes [R][K / 2]      box 128 bytes x 192, 64, 16 rows
-    CUtensorMap tmXs;              // exponents of x [row blocks][KQ][512 bytes]   box 2 row blocks x 2 x 512 bytes
-    const uint8_t *w_scales;
+    CUtensorMap tmWs, tmXs;        // exponents [row blocks][KQ][512 bytes]   box 1 (x: 2) row blocks x 2 x 512 bytes
     const int32_t *offsets;        // [E + 1]
     void *out;
     long long ld_out;              // elements
@@ -317,11 +316,6 @@ __device__ __forceinline__ void tc_kblock_mxf4(uint32_t d_tmem, uint32_t w_lo, u
         "r"(steps), "r"(empty_bar), "r"(kSmemDescHi), "r"(kScaleDescHi)
         : "memory");
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
 {
     asm volatile(
@@ -390,6 +384,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         prefetch_tensormap(&P.tmW);
         prefetch_tensormap(&P.tmX[0]);
+        prefetch_tensormap(&P.tmWs);
         prefetch_tensormap(&P.tmXs);
     }
     if (warp == 1) tmem_alloc(smem_u32(&ctl->tmem_base), kPrTmemCols);
@@ -433,25 +428,24 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     const unsigned long long deadline = globaltimer_ns() + P.wait_ns;
     ProductWalk walk(P, ctl);
 
-    // Two loaders, one thread each: a copy's issue takes its thread about 100 cycles whatever it copies, and with one thread for the seven
-    // copies that a stage then took (x in boxes of 64 rows, exponents of two row blocks) the issue alone was 720 of a stage's 1100 cycles.
+    // Two loaders, one thread each, two copies a stage.  A tiled copy's issue takes its thread about 80 cycles whatever it brings, an
+    // untiled one 350: with one thread for the four tiled and three untiled copies that a stage once took (x in boxes of 64 rows, the
+    // exponents of every row block by themselves) the issue alone was 720 of a stage's 1100 cycles.
     if (warp == 0) {
         if (lane == 0) {
             int stage = 0;
             uint32_t phase = 0, armed = 0;
             bool ok = true;
-            const long long row_bytes = (long long)P.KQ * kMxTileBytes;
             for (; walk.g < total && ok; walk.next()) {
                 const ProductTile t = walk.tile(P, ctl);
-                const uint8_t *ws = P.w_scales + ((long long)t.e * P.N / kMxTile + t.e + t.n0 / kMxTile) * row_bytes;
-                for (int kb = 0; kb < P.num_kb; ++kb, ws += 2 * kMxTileBytes) {
+                const int block = t.e * P.N / kMxTile + t.e + t.n0 / kMxTile;
+                for (int kb = 0; kb < P.num_kb; ++kb) {
                     ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 70u);
                     if (!ok) break;
                     const uint32_t bar = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * kPrStageBytes);
-                    const uint32_t sb = (uint32_t)min(2, P.KQ - 2 * kb) * kMxTileBytes;      // exponents that there are
-                    mbar_arrive_expect_tx(bar, kPrWBytes + sb);
+                    mbar_arrive_expect_tx(bar, kPrWBytes + kPrWScaleBytes);
                     tma_load_3d(dst, &P.tmW, bar, kb * (kPrK / 2), t.n0, t.e);
-                    bulk_load(dst + kPrWBytes + kPrXBytes, ws, sb, bar);
+                    tma_load_3d(dst + kPrWBytes + kPrXBytes, &P.tmWs, bar, 0, 2 * kb, block);
                     armed |= 1u << stage;
                     if (++stage == kPrStages) { stage = 0; phase ^= 1u; }
                 }
@@ -676,7 +670,6 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     if (const int32_t rc = require_handle_device(h, "moe_mxfp4_gemm")) return rc;
     ProductParams p;
     memset(&p, 0, sizeof p);
-    p.w_scales = static_cast<const uint8_t *>(w_scales);
     p.offsets = offsets;
     p.out = out;
     p.ld_out = ld_out;
@@ -694,7 +687,8 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     if (tiles >= (int64_t)1 << 31) return MOE_ERR_SHAPE;
     if (!code_map(h, &p.tmW, w_codes, E_tot, N, K / 2, kPrN, "w_codes") || !code_map(h, &p.tmX[0], x_codes, 0, rows, K / 2, kPrRows, "x_codes") ||
         !code_map(h, &p.tmX[1], x_codes, 0, rows, K / 2, 64, "x_codes") || !code_map(h, &p.tmX[2], x_codes, 0, rows, K / 2, 16, "x_codes") ||
-        !scale_map(h, &p.tmXs, x_scales, scale_blocks(rows, E_tot), p.KQ, "x_scales"))
+        !scale_map(h, &p.tmXs, x_scales, scale_blocks(rows, E_tot), p.KQ, 2, "x_scales") ||
+        !scale_map(h, &p.tmWs, w_scales, scale_blocks((int64_t)E_tot * N, E_tot), p.KQ, 1, "w_scales"))
         return MOE_ERR_CUDA;
     const unsigned grid = (unsigned)(tiles < h->G ? tiles : h->G);
     const cudaError_t err = launch_chained(dtype == MOE_BF16 ? mxfp4_product_kernel<__nv_bfloat16> : mxfp4_product_kernel<__half>, grid, kPrThreads, kPrSmem,
