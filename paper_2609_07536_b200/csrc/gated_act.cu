@@ -6,8 +6,8 @@
 // which values up to an eighth beyond 448 would saturate).  The scaling is exact, so that a value's one rounding is the
 // code's, half a step of 2^-3 of it.  A value that is infinite or no number becomes the code for no number, alone.
 // Bound by HBM: 2 I elements in, I out, 2 I + I / 16 bytes of copy; the backward pass reads I elements and the copy and writes 2 I
-// elements (and the I of act, which the gradient of the next weights needs and which is not kept).  A thread has 8 columns of
-// gate and the same of up, four threads share an exponent by shuffles.
+// elements (and the I of act, which the gradient of the next weights needs and which is not kept).  A thread has 16 (backward
+// pass: 8) columns of gate and the same of up.
 
 #include <cuda_fp8.h>
 
@@ -22,8 +22,8 @@ constexpr int kActThreads = 256;
 struct GatedAct {
     long long ld_in, ld_act, ld_d_act, ld_out;   // elements: gate_up, act, d_act, d_gate_up
     uint8_t *codes, *scales;
-    int32_t rows, I, lanes;            // lanes: threads of a row, 4 per 32 columns
-    int32_t rows_per_cta;
+    int32_t rows, I, lanes;            // lanes: threads of a row, two per 32 columns (backward pass: four)
+    int32_t rows_per_cta, wide;        // wide: 16 columns of the matrices are on 32-byte boundaries
     Divisor by_lanes;
 };
 
@@ -33,28 +33,40 @@ __device__ __forceinline__ float exp_of(float x) { return sizeof(E) == 4 ? expf(
 template <class E>
 __device__ __forceinline__ float ratio(float a, float b) { return sizeof(E) == 4 ? a / b : __fdividef(a, b); }
 
-// eight codes of x * 2^-e, x = 0 .. 448 * 2^e in magnitude
-__device__ __forceinline__ uint2 e4m3_codes(const float (&x)[8], int e, uint32_t bad)
+// sixteen codes of x * 2^-e, x = 0 .. 448 * 2^e in magnitude
+__device__ __forceinline__ uint4 e4m3_codes(const float (&x)[16], int e)
 {
     const float inv = power_of_two(-e);
-    uint32_t w[2];
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i] * inv, x[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
         const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2] * inv, x[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
         w[i] = lo | (hi << 16);
     }
-    if (bad) {
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Where a value is not finite: the largest finite magnitude, and the code for no number in the place of such values
+__device__ __forceinline__ float finite_magnitude(const float (&x)[16])
+{
+    float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (bad >> i & 1u) w[i >> 2] |= 0x7Fu << (8 * (i & 3));
-    }
-    return make_uint2(w[0], w[1]);
+    for (int i = 0; i < 16; ++i)
+        if (fabsf(x[i]) <= 3.402823466e38f) m = fmaxf(m, fabsf(x[i]));
+    return m;
+}
+__device__ __forceinline__ uint4 mark_not_finite(const float (&x)[16], uint4 codes)
+{
+    uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (!(fabsf(x[i]) <= 3.402823466e38f)) w[i >> 2] |= 0x7Fu << (8 * (i & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // the exponent for a largest magnitude: smallest e >= -127 with amax <= 448 * 2^e = 1.75 * 2^(e + 8)
-__device__ __forceinline__ int e4m3_exponent(float amax)
+__device__ __forceinline__ int e4m3_exponent(uint32_t amax_bits)
 {
-    return max(-127, (int)((__float_as_uint(amax) + 0x1FFFFFu) >> 23) - 127 - 8);
+    return max(-127, (int)((amax_bits + 0x1FFFFFu) >> 23) - 127 - 8);
 }
 __device__ __forceinline__ void e4m3_values(uint2 c, float scale, float (&x)[8])
 {
@@ -68,8 +80,11 @@ __device__ __forceinline__ void e4m3_values(uint2 c, float scale, float (&x)[8])
     }
 }
 
+// Two threads share the exponents of 32 columns.  What costs besides the bytes is the issue of the instructions that make the copy: a
+// thread takes 16 columns, so that addresses and exponents are worked out once for them, and finds its largest magnitudes in the
+// 16-bit patterns, two values a step.
 template <class E, bool kKeep>
-__global__ void __launch_bounds__(kActThreads) gated_act_kernel(GatedAct p, const E *gate_up, E *act)
+__global__ void __launch_bounds__(kActThreads, 4) gated_act_kernel(const __grid_constant__ GatedAct p, const E *gate_up, E *act)
 {
     grid_dependency_wait();
     const long long row0 = (long long)blockIdx.x * p.rows_per_cta;
@@ -77,34 +92,52 @@ __global__ void __launch_bounds__(kActThreads) gated_act_kernel(GatedAct p, cons
     for (int base = (int)(threadIdx.x & ~31u); base < items; base += kActThreads) {
         const int it = base + (int)(threadIdx.x & 31u), r = quotient(p.by_lanes, it), q = it - r * p.lanes;
         const long long row = row0 + r;
-        const bool live = it < items && q * 8 < p.I;
-        float g[8], u[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = u[i] = 0.0f;
+        const bool live = it < items && q * 16 < p.I;
+        Raw16<E> rg = {}, ru = {};
+        float g[16], u[16];
         if (live) {
-            const E *src = gate_up + row * p.ld_in + q * 8;
-            load8<E>(src, g);
-            load8<E>(src + p.I, u);
-            float y[8];
+            const E *src = gate_up + row * p.ld_in + q * 16;
+            load16<E>(src, p.wide, rg);
+            load16<E>(src + p.I, p.wide, ru);
+        }
+        values16<E>(rg, g);
+        values16<E>(ru, u);
+        if (live) {
+            float y[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = ratio<E>(g[i], 1.0f + exp_of<E>(-g[i])) * u[i];
-            store8<E>(act + row * p.ld_act + q * 8, y);
+            for (int i = 0; i < 16; ++i) y[i] = ratio<E>(g[i], 1.0f + exp_of<E>(-g[i])) * u[i];
+            store16<E>(act + row * p.ld_act + q * 16, p.wide, y);
         }
         if (!kKeep) continue;
-        uint32_t bad_g, bad_u;
-        float mg = finite_amax8(g, bad_g), mu = finite_amax8(u, bad_u);
-#pragma unroll
-        for (int m = 1; m < 4; m *= 2) {
-            mg = fmaxf(mg, __shfl_xor_sync(0xffffffffu, mg, m));
-            mu = fmaxf(mu, __shfl_xor_sync(0xffffffffu, mu, m));
+        uint32_t mg = magnitude16<E>(rg), mu = magnitude16<E>(ru);
+        if constexpr (sizeof(E) == 2) {
+            uint32_t both = mg | (mu << 16);
+            both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 1));
+            mg = both & 0xffffu;
+            mu = both >> 16;
+        } else {
+            mg = max(mg, __shfl_xor_sync(0xffffffffu, mg, 1));
+            mu = max(mu, __shfl_xor_sync(0xffffffffu, mu, 1));
+        }
+        uint32_t bg = magnitude_bits<E>(mg), bu = magnitude_bits<E>(mu);
+        const bool hurt = mg >= kNotFinite<E> || mu >= kNotFinite<E>;
+        if (__any_sync(0xffffffffu, hurt)) {
+            float fg = finite_magnitude(g), fu = finite_magnitude(u);
+            bg = __float_as_uint(fmaxf(fg, __shfl_xor_sync(0xffffffffu, fg, 1)));
+            bu = __float_as_uint(fmaxf(fu, __shfl_xor_sync(0xffffffffu, fu, 1)));
         }
         if (!live) continue;
-        const int eg = e4m3_exponent(mg), eu = e4m3_exponent(mu), blocks = p.lanes >> 2;
-        uint8_t *c = p.codes + row * 2 * p.I + q * 8;
-        *reinterpret_cast<uint2 *>(c) = e4m3_codes(g, eg, bad_g);
-        *reinterpret_cast<uint2 *>(c + p.I) = e4m3_codes(u, eu, bad_u);
-        if ((q & 3) == 0) {
-            uint8_t *sc = p.scales + row * 2 * blocks + (q >> 2);
+        const int eg = e4m3_exponent(bg), eu = e4m3_exponent(bu), blocks = p.lanes >> 1;
+        uint4 cg = e4m3_codes(g, eg), cu = e4m3_codes(u, eu);
+        if (hurt) {
+            cg = mark_not_finite(g, cg);
+            cu = mark_not_finite(u, cu);
+        }
+        uint8_t *c = p.codes + row * 2 * p.I + q * 16;
+        st_row_v4(c, cg);
+        st_row_v4(c + p.I, cu);
+        if ((q & 1) == 0) {
+            uint8_t *sc = p.scales + row * 2 * blocks + (q >> 1);
             sc[0] = (uint8_t)(eg + 127);
             sc[blocks] = (uint8_t)(eu + 127);
         }
@@ -112,7 +145,7 @@ __global__ void __launch_bounds__(kActThreads) gated_act_kernel(GatedAct p, cons
 }
 
 template <class E>
-__global__ void __launch_bounds__(kActThreads) gated_act_grad_kernel(GatedAct p, const E *d_act, E *d_gate_up, E *act)
+__global__ void __launch_bounds__(kActThreads) gated_act_grad_kernel(const __grid_constant__ GatedAct p, const E *d_act, E *d_gate_up, E *act)
 {
     grid_dependency_wait();
     const long long row0 = (long long)blockIdx.x * p.rows_per_cta;
@@ -145,12 +178,12 @@ __global__ void __launch_bounds__(kActThreads) gated_act_grad_kernel(GatedAct p,
 
 bool sizes_ok(int32_t rows, int32_t I) { return rows >= 0 && rows < 1 << 30 && I >= 16 && I % 16 == 0 && I <= 1 << 20; }
 
-GatedAct describe(const moe_handle *h, int32_t rows, int32_t I)
+GatedAct describe(const moe_handle *h, int32_t rows, int32_t I, int lanes_per_block)
 {
     GatedAct p = {};
     p.rows = rows;
     p.I = I;
-    p.lanes = (I + 31) / 32 * 4;
+    p.lanes = (I + 31) / 32 * lanes_per_block;
     p.by_lanes = divisor_of(p.lanes);
     // 16 rows a block fill its passes of 256 threads to within a row; fewer where that leaves SMs without a block
     p.rows_per_cta = 16;
@@ -174,7 +207,8 @@ extern "C" int32_t moe_gated_act(moe_handle *h, const void *gate_up, int64_t ld_
     if (!gate_up || !act || !codes_or_null != !scales_or_null) return MOE_ERR_NULL;
     if (!rows_aligned(gate_up) || !rows_aligned(act) || !rows_aligned(codes_or_null)) return MOE_ERR_ALIGN;
     if (const int32_t rc = require_handle_device(h, "moe_gated_act")) return rc;
-    GatedAct p = describe(h, rows, I);
+    GatedAct p = describe(h, rows, I, 2);
+    p.wide = rows_wide(gate_up, ld_gate_up, dtype) && rows_wide(act, ld_act, dtype);
     p.ld_in = ld_gate_up;
     p.ld_act = ld_act;
     p.codes = static_cast<uint8_t *>(codes_or_null);
@@ -201,7 +235,7 @@ extern "C" int32_t moe_gated_act_grad(moe_handle *h, const void *d_act, int64_t 
     if (!d_act || !codes || !scales || !d_gate_up) return MOE_ERR_NULL;
     if (!rows_aligned(d_act) || !rows_aligned(codes) || !rows_aligned(d_gate_up) || !rows_aligned(act_or_null)) return MOE_ERR_ALIGN;
     if (const int32_t rc = require_handle_device(h, "moe_gated_act_grad")) return rc;
-    GatedAct p = describe(h, rows, I);
+    GatedAct p = describe(h, rows, I, 4);
     p.ld_act = ld_act;
     p.ld_d_act = ld_d_act;
     p.ld_out = ld_d_gate_up;
