@@ -170,32 +170,42 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
 //
 // out[r][n] = sum_k x[r][k] w[e][n][k] for the rows r of expert e, fp32 accumulation in TMEM, one rounding at the end.
 // The weights are on the M side of the MMA and the rows on its N side, as in the other products here: a tile costs what its rows cost.
-// Tile: 128 columns of the output x up to 192 rows.  TMEM holds two accumulators of 192 columns and, for every operand stage, 24
-// columns of exponents (128 rows of weights: 4 per 128 columns of K; 256 rows of x: 8); that is 504 of its 512 columns, and why a
-// tile has 192 rows and not 256.  A stage is 256 columns of K: 128 bytes of codes a row, a swizzle row.
+// Tile: 128 columns of the output x up to 192 rows, or, computed by a pair of CTAs (cta_group::2), 256 columns x up to 192 rows: each CTA
+// then loads its own 128 rows of the weights and half of the rows of x, 31 KB a stage instead of 43 for the same products.
+// TMEM holds two accumulators of 192 columns and, for five stages, 24 columns of exponents (128 rows of weights: 4 per 128
+// columns of K; 256 rows of x: 8; a pair's CTAs each have those of all rows of x); that is 504 of its 512 columns, and why a tile has
+// 192 rows and not 256.  A stage is 256 columns of K: 128 bytes of codes a row, a swizzle row.
 //   warps 0, 2  loaders (one thread each): codes of the weights, of the rows, and their exponents as they lie;
 //   warp 1      copies the exponents to TMEM (tcgen05.cp, each of the four lane quarters gets them) and issues
 //               tcgen05.mma.kind::mxf4.block_scale (K = 64, two exponents a row); both are issued by one lane of the converged
-//               warp and run in order;
+//               warp (pair: of the first CTA) and run in order;
 //   warps 4-11  epilogue: pieces of 32 rows x 32 columns, 16-bit, transposed in registers, 64 contiguous bytes a row.
 
 constexpr int kPrThreads = 384, kPrEpiWarps = 8;
-constexpr int kPrN = 128;                                   // output columns of a tile (M of the MMA)
+constexpr int kPrN = 128;                                   // output columns of a CTA's part of a tile (M of the MMA: a pair's twice that)
 constexpr int kPrRows = 192;                                // rows of a tile (N of the MMA)
 constexpr int kPrK = 256, kPrStepK = 64;                    // columns of K of a stage, of an MMA
-constexpr int kPrStages = 5;
-constexpr int kPrWBytes = kPrN * kPrK / 2, kPrXBytes = kPrRows * kPrK / 2;
+constexpr int kPrWBytes = kPrN * kPrK / 2;
 constexpr int kPrWScaleBytes = 2 * kMxTileBytes, kPrXScaleBytes = 4 * kMxTileBytes;      // x: row block 0 of both 128s of K, then row block 1
-constexpr int kPrStageBytes = kPrWBytes + kPrXBytes + kPrWScaleBytes + kPrXScaleBytes;
-constexpr int kPrScaleCols = 24;                            // TMEM columns of a stage's exponents: weights 2 x 4, rows 2 x 8
+constexpr int kPrScaleCols = 24, kPrScaleBuffers = 5;       // TMEM columns of a stage's exponents: weights 2 x 4, rows 2 x 8
 constexpr int kPrTmemCols = 512;
+constexpr int kPrMaxStages = 7;
 constexpr int kMaxExperts = 1024;
-static_assert(2 * kPrRows + kPrStages * kPrScaleCols <= kPrTmemCols, "accumulators and exponents exceed TMEM");
-static_assert(kPrStageBytes % 1024 == 0, "stages are 1024-byte aligned");
+template <bool kPair>
+struct PrCfg {
+    static constexpr int kTileN = kPair ? 2 * kPrN : kPrN;
+    static constexpr int kXRows = kPair ? kPrRows / 2 : kPrRows;                         // rows of x that a CTA holds
+    static constexpr int kXBytes = kXRows * kPrK / 2;
+    static constexpr int kStageBytes = kPrWBytes + kXBytes + kPrWScaleBytes + kPrXScaleBytes;
+    static constexpr int kStages = kPair ? 7 : 5;
+    static constexpr int kRound = kPair ? 32 : 16;                                       // N of the MMA is a multiple of this
+    static_assert(kStageBytes % 1024 == 0 && kStages <= kPrMaxStages, "stages are 1024-byte aligned");
+};
+static_assert(2 * kPrRows + kPrScaleBuffers * kPrScaleCols <= kPrTmemCols, "accumulators and exponents exceed TMEM");
 
 struct alignas(64) ProductParams {
     CUtensorMap tmW;               // codes [E][N][K / 2]   box 128 bytes x 128 rows, 128B swizzle
-    CUtensorMap tmX[3];            // codes [R][K / 2]      box 128 bytes x 192, 64, 16 rows
+    CUtensorMap tmX[3];            // codes [R][K / 2]      box 128 bytes x 192, 64, 16 rows (pair: 96, 32, unused)
     CUtensorMap tmWs, tmXs;        // exponents [row blocks][KQ][512 bytes]   box 1 (x: 2) row blocks x 2 x 512 bytes
     const int32_t *offsets;        // [E + 1]
     void *out;
@@ -206,7 +216,7 @@ struct alignas(64) ProductParams {
     Divisor by_NT;
 };
 struct ProductControl {
-    unsigned long long full[kPrStages], empty[kPrStages], tmem_full[2], tmem_empty[2], drain;
+    unsigned long long full[kPrMaxStages], empty[kPrMaxStages], tmem_full[2], tmem_empty[2], drain;
     uint32_t tmem_base;
     volatile uint32_t abort;
     int32_t first[kMaxExperts + 1];       // row where an expert's rows begin
@@ -231,21 +241,22 @@ __device__ __forceinline__ bool pr_wait(uint32_t bar, uint32_t parity, ProductCo
     return true;
 }
 
-// The tiles of a CTA: row tile outer, column tile inner, every gridDim.x-th one.  The expert is found by a vote of the warp for the first
+// The tiles of a CTA (of a pair): row tile outer, column tile inner, dealt one by one.  The expert is found by a vote of the warp for the first
 // tile and by steps from there on (found by bisection for every tile, and the addresses worked out from nothing, a tile's start cost
 // 1500 cycles in every role, of 9000 that a tile of 2048 columns took).
 struct ProductTile {
     int e, row0, valid, local, n0;     // local: first row inside the expert
 };
+template <bool kPair>
 struct ProductWalk {
     int g, e;
     // (the whole warp)
-    __device__ __forceinline__ ProductWalk(const ProductParams &P, const ProductControl *ctl) : g((int)blockIdx.x), e(-1)
+    __device__ __forceinline__ ProductWalk(const ProductParams &P, const ProductControl *ctl) : g((int)blockIdx.x >> (kPair ? 1 : 0)), e(-1)
     {
         const int mu = quotient(P.by_NT, g), lane = threadIdx.x & 31;
         for (int i = 0; i < P.E; i += 32) e += __popc(__ballot_sync(0xffffffffu, i + lane < P.E && ctl->tiles[i + lane] <= mu));
     }
-    __device__ __forceinline__ void next() { g += (int)gridDim.x; }
+    __device__ __forceinline__ void next() { g += (int)gridDim.x >> (kPair ? 1 : 0); }
     __device__ __forceinline__ ProductTile tile(const ProductParams &P, const ProductControl *ctl)
     {
         const int mu = quotient(P.by_NT, g);
@@ -255,71 +266,78 @@ struct ProductWalk {
         t.local = (mu - ctl->tiles[e]) * kPrRows;
         t.row0 = ctl->first[e] + t.local;
         t.valid = min(kPrRows, ctl->first[e + 1] - t.row0);
-        t.n0 = (g - mu * P.NT) * kPrN;
+        t.n0 = (g - mu * P.NT) * PrCfg<kPair>::kTileN;
         return t;
     }
 };
 
-// Instruction descriptor, kind::mxf4: e2m1 operands, K-major, M = 128, exponents of type ue8m0, exponent pair `half` of the column's four bytes
-__device__ __forceinline__ uint32_t mxf4_idesc(uint32_t n, uint32_t half)
+// Instruction descriptor, kind::mxf4: e2m1 operands, K-major, M x N, exponents of type ue8m0, exponent pair `half` of the column's four bytes
+__device__ __forceinline__ uint32_t mxf4_idesc(uint32_t m, uint32_t n, uint32_t half)
 {
-    return (2u * half << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((uint32_t)(kPrN >> 4) << 24) | (2u * half << 29);
+    return (2u * half << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24) | (2u * half << 29);
 }
 // Exponents, shared memory -> TMEM: 512 contiguous bytes are 32 rows of 16, which become 32 lanes x 4 columns in each of the four lane
 // quarters.  Descriptor: no swizzle, eights of rows 128 bytes apart (stride offset), version 1.
 constexpr uint32_t kScaleDescHi = (128u >> 4) | (1u << 14);
 __device__ __forceinline__ uint32_t scale_desc_lo(uint32_t smem) { return ((smem & 0x3FFFFu) >> 4) | (1u << 16); }
 // One stage of operands in one statement: the exponents' copies (`two`: two row blocks of x), `steps` MMAs and the commit that hands the
-// stage back.  All of them are issued by one thread and run in order.
-__device__ __forceinline__ void tc_kblock_mxf4(uint32_t d_tmem, uint32_t w_lo, uint32_t x_lo, uint32_t ws_lo, uint32_t xs_lo, uint32_t sw, uint32_t sx,
-                                               uint32_t shift, uint32_t two, uint32_t idesc0, uint32_t idesc1, uint32_t accumulate, uint32_t steps,
-                                               uint32_t empty_bar)
+// stage back, to both CTAs of a pair.  All of them are issued by one thread and run in order.  First the exponents of the first 128
+// columns, then of the second; 64 columns of codes are 32 bytes further along the swizzle row.
+#define MOE_MXF4_STAGE(GROUP, COMMIT) \
+    asm volatile( \
+        "{\n\t.reg .pred p, q, t, t1, s1, s2, s3;\n\t.reg .b64 da, db;\n\t.reg .b32 al, bl, sa, sb;\n\t" \
+        "setp.ne.b32 p, %11, 0;\n\t" \
+        "setp.eq.b32 q, %11, %11;\n\t" \
+        "setp.ne.b32 t, %8, 0;\n\t" \
+        "setp.gt.u32 s1, %12, 1;\n\t" \
+        "setp.gt.u32 s2, %12, 2;\n\t" \
+        "setp.gt.u32 s3, %12, 3;\n\t" \
+        "and.pred t1, t, s2;\n\t" \
+        "mov.b64 da, {%3, %15};\n\t" \
+        "tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [%5], da;\n\t" \
+        "mov.b64 da, {%4, %15};\n\t" \
+        "tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [%6], da;\n\t" \
+        "add.u32 al, %4, 64;\n\tadd.u32 sa, %6, 4;\n\t" \
+        "mov.b64 da, {al, %15};\n\t" \
+        "@t tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
+        "add.u32 al, %3, 32;\n\tadd.u32 sa, %5, 4;\n\t" \
+        "mov.b64 da, {al, %15};\n\t" \
+        "@s2 tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
+        "add.u32 al, %4, 32;\n\tadd.u32 sa, %6, 8;\n\t" \
+        "mov.b64 da, {al, %15};\n\t" \
+        "@s2 tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
+        "add.u32 al, %4, 96;\n\tadd.u32 sa, %6, 12;\n\t" \
+        "mov.b64 da, {al, %15};\n\t" \
+        "@t1 tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
+        "add.u32 sb, %6, %7;\n\t" \
+        "mov.b64 da, {%1, %14};\n\tmov.b64 db, {%2, %14};\n\t" \
+        "tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [%5], [sb], p;\n\t" \
+        "add.u32 al, %1, 2;\n\tadd.u32 bl, %2, 2;\n\t" \
+        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t" \
+        "@s1 tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [%5], [sb], q;\n\t" \
+        "add.u32 sa, %5, 4;\n\tadd.u32 sb, sb, 8;\n\t" \
+        "add.u32 al, %1, 4;\n\tadd.u32 bl, %2, 4;\n\t" \
+        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t" \
+        "@s2 tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [sa], [sb], q;\n\t" \
+        "add.u32 al, %1, 6;\n\tadd.u32 bl, %2, 6;\n\t" \
+        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t" \
+        "@s3 tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [sa], [sb], q;\n\t" \
+        COMMIT "\n\t}" \
+        ::"r"(d_tmem), "r"(w_lo), "r"(x_lo), "r"(ws_lo), "r"(xs_lo), "r"(sw), "r"(sx), "r"(shift), "r"(two), "r"(idesc0), "r"(idesc1), "r"(accumulate), \
+        "r"(steps), "r"(empty_bar), "r"(kSmemDescHi), "r"(kScaleDescHi), "h"((uint16_t)3) \
+        : "memory")
+template <bool kPair>
+__device__ __forceinline__ void tc_stage_mxf4(uint32_t d_tmem, uint32_t w_lo, uint32_t x_lo, uint32_t ws_lo, uint32_t xs_lo, uint32_t sw, uint32_t sx,
+                                              uint32_t shift, uint32_t two, uint32_t idesc0, uint32_t idesc1, uint32_t accumulate, uint32_t steps,
+                                              uint32_t empty_bar)
 {
-    asm volatile(
-        "{\n\t.reg .pred p, q, t, t1, s1, s2, s3;\n\t.reg .b64 da, db;\n\t.reg .b32 al, bl, sa, sb;\n\t"
-        "setp.ne.b32 p, %11, 0;\n\t"
-        "setp.eq.b32 q, %11, %11;\n\t"
-        "setp.ne.b32 t, %8, 0;\n\t"
-        "setp.gt.u32 s1, %12, 1;\n\t"
-        "setp.gt.u32 s2, %12, 2;\n\t"
-        "setp.gt.u32 s3, %12, 3;\n\t"
-        "and.pred t1, t, s2;\n\t"
-        // exponents of the first 128 columns, then of the second
-        "mov.b64 da, {%3, %15};\n\t"
-        "tcgen05.cp.cta_group::1.32x128b.warpx4 [%5], da;\n\t"
-        "mov.b64 da, {%4, %15};\n\t"
-        "tcgen05.cp.cta_group::1.32x128b.warpx4 [%6], da;\n\t"
-        "add.u32 al, %4, 64;\n\tadd.u32 sa, %6, 4;\n\t"
-        "mov.b64 da, {al, %15};\n\t"
-        "@t tcgen05.cp.cta_group::1.32x128b.warpx4 [sa], da;\n\t"
-        "add.u32 al, %3, 32;\n\tadd.u32 sa, %5, 4;\n\t"
-        "mov.b64 da, {al, %15};\n\t"
-        "@s2 tcgen05.cp.cta_group::1.32x128b.warpx4 [sa], da;\n\t"
-        "add.u32 al, %4, 32;\n\tadd.u32 sa, %6, 8;\n\t"
-        "mov.b64 da, {al, %15};\n\t"
-        "@s2 tcgen05.cp.cta_group::1.32x128b.warpx4 [sa], da;\n\t"
-        "add.u32 al, %4, 96;\n\tadd.u32 sa, %6, 12;\n\t"
-        "mov.b64 da, {al, %15};\n\t"
-        "@t1 tcgen05.cp.cta_group::1.32x128b.warpx4 [sa], da;\n\t"
-        // products: 64 columns are 32 bytes further along the swizzle row
-        "add.u32 sb, %6, %7;\n\t"
-        "mov.b64 da, {%1, %14};\n\tmov.b64 db, {%2, %14};\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [%5], [sb], p;\n\t"
-        "add.u32 al, %1, 2;\n\tadd.u32 bl, %2, 2;\n\t"
-        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t"
-        "@s1 tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [%5], [sb], q;\n\t"
-        "add.u32 sa, %5, 4;\n\tadd.u32 sb, sb, 8;\n\t"
-        "add.u32 al, %1, 4;\n\tadd.u32 bl, %2, 4;\n\t"
-        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t"
-        "@s2 tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [sa], [sb], q;\n\t"
-        "add.u32 al, %1, 6;\n\tadd.u32 bl, %2, 6;\n\t"
-        "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t"
-        "@s3 tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [sa], [sb], q;\n\t"
-        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%13];\n\t}"
-        ::"r"(d_tmem), "r"(w_lo), "r"(x_lo), "r"(ws_lo), "r"(xs_lo), "r"(sw), "r"(sx), "r"(shift), "r"(two), "r"(idesc0), "r"(idesc1), "r"(accumulate),
-        "r"(steps), "r"(empty_bar), "r"(kSmemDescHi), "r"(kScaleDescHi)
-        : "memory");
+    if constexpr (kPair) {
+        MOE_MXF4_STAGE("2", "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%13], %16;");
+    } else {
+        MOE_MXF4_STAGE("1", "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%13];");
+    }
 }
+#undef MOE_MXF4_STAGE
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
 {
     asm volatile(
@@ -356,31 +374,34 @@ __device__ __forceinline__ void store_piece(const uint32_t (&lo)[16], const uint
 }
 
 // A loader's wind-down: the copies already issued land before shared memory is released
+template <int kStages>
 __device__ __forceinline__ void pr_drain(ProductControl *ctl, uint32_t armed, int stage, uint32_t phase)
 {
     const unsigned long long drain = globaltimer_ns() + 2000000ull;
-    for (int i = 0; i < kPrStages; ++i) {
+    for (int i = 0; i < kStages; ++i) {
         if (!(armed & (1u << i))) continue;
         const uint32_t par = i < stage ? phase : (phase ^ 1u);
         while (!mbar_try_wait(smem_u32(&ctl->full[i]), par) && globaltimer_ns() < drain) {}
     }
 }
 
-template <class E>
+template <class E, bool kPair>
 __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __grid_constant__ ProductParams P)
 {
+    using C = PrCfg<kPair>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    ProductControl *ctl = reinterpret_cast<ProductControl *>(ring + kPrStages * kPrStageBytes);
+    ProductControl *ctl = reinterpret_cast<ProductControl *>(ring + C::kStages * C::kStageBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = kPair ? cluster_ctarank() : 0u;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kPrStages; ++i) {
-            mbar_init(smem_u32(&ctl->full[i]), 2);            // the two loaders
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(smem_u32(&ctl->full[i]), 2);            // the two loaders (pair: the first CTA's, which arm it for both)
             mbar_init(smem_u32(&ctl->empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&ctl->tmem_full[i]), 1);
-            mbar_init(smem_u32(&ctl->tmem_empty[i]), kPrEpiWarps);
+            mbar_init(smem_u32(&ctl->tmem_empty[i]), (kPair ? 2 : 1) * kPrEpiWarps);
         }
         mbar_init(smem_u32(&ctl->drain), 1);
         ctl->abort = 0u;
@@ -391,7 +412,10 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         prefetch_tensormap(&P.tmWs);
         prefetch_tensormap(&P.tmXs);
     }
-    if (warp == 1) tmem_alloc(smem_u32(&ctl->tmem_base), kPrTmemCols);
+    if (warp == 1) {
+        if (kPair) tmem_alloc_pair(smem_u32(&ctl->tmem_base), kPrTmemCols);
+        else tmem_alloc(smem_u32(&ctl->tmem_base), kPrTmemCols);
+    }
     grid_dependency_wait();
     for (int e = threadIdx.x; e <= P.E; e += kPrThreads) ctl->first[e] = ld_chained(P.offsets + e);
     tc_fence_before();
@@ -427,14 +451,16 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         }
     }
     __syncthreads();
+    if (kPair) cluster_sync_all();     // the other CTA's barriers exist before anything arrives on them
     const uint32_t tmem_base = ctl->tmem_base;
     const int total = ctl->tiles[P.E] * P.NT;
     const unsigned long long deadline = globaltimer_ns() + P.wait_ns;
-    ProductWalk walk(P, ctl);
+    ProductWalk<kPair> walk(P, ctl);
 
     // Two loaders, one thread each, two copies a stage.  A tiled copy's issue takes its thread about 80 cycles whatever it brings, an
     // untiled one 350: with one thread for the four tiled and three untiled copies that a stage once took (x in boxes of 64 rows, the
-    // exponents of every row block by themselves) the issue alone was 720 of a stage's 1100 cycles.
+    // exponents of every row block by themselves) the issue alone was 720 of a stage's 1100 cycles.  Pair: every copy completes on the
+    // first CTA's barrier, at the same offset there.
     if (warp == 0) {
         if (lane == 0) {
             int stage = 0;
@@ -442,19 +468,24 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             bool ok = true;
             for (; walk.g < total && ok; walk.next()) {
                 const ProductTile t = walk.tile(P, ctl);
-                const int block = t.e * P.N / kMxTile + t.e + t.n0 / kMxTile;
+                const int n0 = t.n0 + (int)rank * kPrN, block = t.e * P.N / kMxTile + t.e + n0 / kMxTile;
                 for (int kb = 0; kb < P.num_kb; ++kb) {
                     ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 70u);
                     if (!ok) break;
-                    const uint32_t bar = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * kPrStageBytes);
-                    mbar_arrive_expect_tx(bar, kPrWBytes + kPrWScaleBytes);
-                    tma_load_3d(dst, &P.tmW, bar, kb * (kPrK / 2), t.n0, t.e);
-                    tma_load_3d(dst + kPrWBytes + kPrXBytes, &P.tmWs, bar, 0, 2 * kb, block);
+                    const uint32_t own = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * C::kStageBytes);
+                    if (rank == 0) mbar_arrive_expect_tx(own, (kPair ? 2u : 1u) * (uint32_t)(kPrWBytes + kPrWScaleBytes));
+                    if (kPair) {
+                        tma_load_3d_pair(dst, &P.tmW, own & 0xFEFFFFFFu, kb * (kPrK / 2), n0, t.e);
+                        tma_load_3d_pair(dst + kPrWBytes + C::kXBytes, &P.tmWs, own & 0xFEFFFFFFu, 0, 2 * kb, block);
+                    } else {
+                        tma_load_3d(dst, &P.tmW, own, kb * (kPrK / 2), n0, t.e);
+                        tma_load_3d(dst + kPrWBytes + C::kXBytes, &P.tmWs, own, 0, 2 * kb, block);
+                    }
                     armed |= 1u << stage;
-                    if (++stage == kPrStages) { stage = 0; phase ^= 1u; }
+                    if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
                 }
             }
-            if (!ok) pr_drain(ctl, armed, stage, phase);
+            if (!ok && rank == 0) pr_drain<C::kStages>(ctl, armed, stage, phase);
         }
         __syncwarp();
     } else if (warp == 2) {
@@ -464,30 +495,36 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             bool ok = true;
             for (; walk.g < total && ok; walk.next()) {
                 const ProductTile t = walk.tile(P, ctl);
-                // 192 rows, or 64s of them, or 16: the rows behind the tile's own are read for nothing
-                const int which = t.valid > 2 * 64 ? 0 : t.valid > 16 ? 1 : 2, boxes = which == 1 && t.valid > 64 ? 2 : 1;
-                const uint32_t box_bytes = (which == 0 ? kPrRows : which == 1 ? 64u : 16u) * (kPrK / 2);
+                // rows that this CTA holds of the tile: in one box, or in two of 64; those behind the tile's own are read for nothing
+                const int held = kPair ? ((t.valid + C::kRound - 1) & -C::kRound) / 2 : t.valid, row0 = t.row0 + (int)rank * held;
+                const int which = kPair ? (held > 32 ? 0 : 1) : held > 128 ? 0 : held > 16 ? 1 : 2, boxes = !kPair && which == 1 && held > 64 ? 2 : 1;
+                const uint32_t box_bytes = (which == 0 ? C::kXRows : which == 1 ? (kPair ? 32u : 64u) : 16u) * (kPrK / 2);
                 const CUtensorMap *map = &P.tmX[which];
                 // the row block that the quantisation put the tile's first row into: by the expert's first row (row0 - local)
                 const int block = (t.row0 - t.local) / kMxTile + t.e + t.local / kMxTile;
                 for (int kb = 0; kb < P.num_kb; ++kb) {
                     ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 74u);
                     if (!ok) break;
-                    const uint32_t bar = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * kPrStageBytes) + kPrWBytes;
-                    mbar_arrive_expect_tx(bar, (uint32_t)boxes * box_bytes + kPrXScaleBytes);
-                    tma_load_2d(dst, map, bar, kb * (kPrK / 2), t.row0);
-                    if (boxes == 2) tma_load_2d(dst + box_bytes, map, bar, kb * (kPrK / 2), t.row0 + 64);
-                    tma_load_3d(dst + kPrXBytes + kPrWScaleBytes, &P.tmXs, bar, 0, 2 * kb, block);
+                    const uint32_t own = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * C::kStageBytes) + kPrWBytes;
+                    if (rank == 0) mbar_arrive_expect_tx(own, (kPair ? 2u : 1u) * ((uint32_t)boxes * box_bytes + kPrXScaleBytes));
+                    if (kPair) {
+                        tma_load_2d_pair(dst, map, own & 0xFEFFFFFFu, kb * (kPrK / 2), row0);
+                        tma_load_3d_pair(dst + C::kXBytes + kPrWScaleBytes, &P.tmXs, own & 0xFEFFFFFFu, 0, 2 * kb, block);
+                    } else {
+                        tma_load_2d(dst, map, own, kb * (kPrK / 2), row0);
+                        if (boxes == 2) tma_load_2d(dst + box_bytes, map, own, kb * (kPrK / 2), row0 + 64);
+                        tma_load_3d(dst + C::kXBytes + kPrWScaleBytes, &P.tmXs, own, 0, 2 * kb, block);
+                    }
                     armed |= 1u << stage;
-                    if (++stage == kPrStages) { stage = 0; phase ^= 1u; }
+                    if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
                 }
             }
-            if (!ok) pr_drain(ctl, armed, stage, phase);
+            if (!ok && rank == 0) pr_drain<C::kStages>(ctl, armed, stage, phase);
         }
         __syncwarp();
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
         // the whole warp runs the loop, converged, and one elected lane issues: warp-uniform operands (see the other products)
-        int stage = 0, it = 0;
+        int stage = 0, it = 0, buffer = 0, early = 0;
         uint32_t phase = 0;
         bool ok = true;
         const uint32_t ring0 = smem_u32(ring), lo0 = smem_desc_lo(ring0), sc0 = scale_desc_lo(ring0), full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
@@ -495,8 +532,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             const ProductTile t = walk.tile(P, ctl);
             const int a = it & 1;
             const uint32_t shift = (uint32_t)(t.local & (kMxTile - 1)) >> 5;                 // 0 or 2 columns: first row inside its row block
-            const uint32_t n = __reduce_max_sync(0xffffffffu, (uint32_t)((t.valid + 15) & ~15)), two = 32u * shift + n > (uint32_t)kMxTile ? 1u : 0u;
-            const uint32_t idesc0 = mxf4_idesc(n, 0u), idesc1 = mxf4_idesc(n, 1u);
+            const uint32_t n = __reduce_max_sync(0xffffffffu, (uint32_t)((t.valid + C::kRound - 1) & -C::kRound)), two = 32u * shift + n > (uint32_t)kMxTile ? 1u : 0u;
+            const uint32_t idesc0 = mxf4_idesc((uint32_t)C::kTileN, n, 0u), idesc1 = mxf4_idesc((uint32_t)C::kTileN, n, 1u);
             ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), ((uint32_t)(it >> 1) & 1u) ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 71u));
             if (!ok) break;
             tc_fence_after();
@@ -504,22 +541,40 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             for (int kb = 0; kb < P.num_kb; ++kb) {
                 ok = __all_sync(0xffffffffu, pr_wait(full0 + 8u * stage, phase, ctl, deadline, P.status, (uint32_t)walk.g, 72u));
                 if (!ok) break;
+                if (C::kStages > kPrScaleBuffers) {
+                    // the exponents' columns are used again after fewer stages than the operands: the MMAs that read them last are done
+                    if (early < kPrScaleBuffers) {
+                        ++early;
+                    } else {
+                        const int then = stage >= kPrScaleBuffers ? stage - kPrScaleBuffers : stage + C::kStages - kPrScaleBuffers;
+                        const uint32_t parity = stage >= kPrScaleBuffers ? phase : phase ^ 1u;
+                        ok = __all_sync(0xffffffffu, pr_wait(empty0 + 8u * then, parity, ctl, deadline, P.status, (uint32_t)walk.g, 75u));
+                        if (!ok) break;
+                    }
+                }
                 tc_fence_after();
                 if (elect_one_sync()) {
-                    constexpr uint32_t kX = kPrWBytes >> 4, kWs = (kPrWBytes + kPrXBytes) >> 4, kXs = kWs + (kPrWScaleBytes >> 4);
-                    const uint32_t w_lo = lo0 + (uint32_t)(stage * (kPrStageBytes >> 4)), s_lo = sc0 + (uint32_t)(stage * (kPrStageBytes >> 4));
-                    const uint32_t sw = tmem_base + (uint32_t)(2 * kPrRows + stage * kPrScaleCols);
-                    tc_kblock_mxf4(d_tmem, w_lo, w_lo + kX, s_lo + kWs, s_lo + kXs, sw, sw + 8u, shift, two, idesc0, idesc1, kb > 0 ? 1u : 0u,
-                                   kb == P.num_kb - 1 ? (uint32_t)P.last_steps : 4u, empty0 + 8u * stage);
-                    if (kb == P.num_kb - 1) tc_commit(smem_u32(&ctl->tmem_full[a]));
+                    constexpr uint32_t kX = kPrWBytes >> 4, kWs = (kPrWBytes + C::kXBytes) >> 4, kXs = kWs + (kPrWScaleBytes >> 4);
+                    const uint32_t w_lo = lo0 + (uint32_t)(stage * (C::kStageBytes >> 4)), s_lo = sc0 + (uint32_t)(stage * (C::kStageBytes >> 4));
+                    const uint32_t sw = tmem_base + (uint32_t)(2 * kPrRows + buffer * kPrScaleCols);
+                    tc_stage_mxf4<kPair>(d_tmem, w_lo, w_lo + kX, s_lo + kWs, s_lo + kXs, sw, sw + 8u, shift, two, idesc0, idesc1, kb > 0 ? 1u : 0u,
+                                         kb == P.num_kb - 1 ? (uint32_t)P.last_steps : 4u, empty0 + 8u * stage);
+                    if (kb == P.num_kb - 1) {
+                        if (kPair) tc_commit_pair(smem_u32(&ctl->tmem_full[a]));
+                        else tc_commit(smem_u32(&ctl->tmem_full[a]));
+                    }
                 }
                 __syncwarp();
-                if (++stage == kPrStages) { stage = 0; phase ^= 1u; }
+                if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+                if (++buffer == kPrScaleBuffers) buffer = 0;
             }
         }
         if (!ok) {
             // what was issued finishes before shared memory and TMEM are released
-            if (elect_one_sync()) tc_commit(smem_u32(&ctl->drain));
+            if (elect_one_sync()) {
+                if (kPair) tc_commit_pair(smem_u32(&ctl->drain));
+                else tc_commit(smem_u32(&ctl->drain));
+            }
             __syncwarp();
             const unsigned long long until = globaltimer_ns() + 2000000ull;
             while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < until) {}
@@ -530,7 +585,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         int it = 0;
         for (; walk.g < total; walk.next(), ++it) {
             const ProductTile t = walk.tile(P, ctl);
-            const int a = it & 1, pieces = (t.valid + 31) >> 5, col = t.n0 + q4 * 32, cols = P.N - col;
+            const int a = it & 1, pieces = (t.valid + 31) >> 5, col = t.n0 + (int)rank * kPrN + q4 * 32, cols = P.N - col;
             uint32_t ok = 1u;
             if (lane == 0) ok = pr_wait(smem_u32(&ctl->tmem_full[a]), (uint32_t)(it >> 1) & 1u, ctl, deadline, P.status, (uint32_t)walk.g, 73u) ? 1u : 0u;
             if (!__shfl_sync(0xffffffffu, ok, 0)) break;
@@ -539,7 +594,10 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             const auto release = [&]() {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&ctl->tmem_empty[a]));
+                if (lane == 0) {
+                    if (kPair) mbar_arrive_cluster_relaxed(mapa_u32(smem_u32(&ctl->tmem_empty[a]), 0u));   // the first CTA's barrier
+                    else mbar_arrive(smem_u32(&ctl->tmem_empty[a]));
+                }
             };
             if (grp >= pieces) release();
 #pragma unroll 1
@@ -556,16 +614,22 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             }
         }
     }
+    // (pair: nobody leaves while the other CTA may still touch its memory)
     tc_fence_before();
     __syncthreads();
+    if (kPair) cluster_sync_all();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, kPrTmemCols);
+        if (kPair) tmem_dealloc_pair(tmem_base, kPrTmemCols);
+        else tmem_dealloc(tmem_base, kPrTmemCols);
     }
 }
 
-constexpr size_t kPrSmem = (size_t)kPrStages * kPrStageBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127);
-static_assert(kPrSmem <= 227 * 1024, "the product's stages exceed the shared memory of an SM");
+template <bool kPair>
+constexpr size_t pr_smem_bytes() { return (size_t)PrCfg<kPair>::kStages * PrCfg<kPair>::kStageBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127); }
+static_assert(pr_smem_bytes<false>() <= 227 * 1024 && pr_smem_bytes<true>() <= 227 * 1024, "the product's stages exceed the shared memory of an SM");
+
+constexpr int32_t kPairRowsPerExpert = 64;
 
 bool columns_ok(int32_t K) { return K >= kMxBlock && K % kMxBlock == 0 && K <= 1 << 20; }
 int64_t scale_blocks(int64_t rows, int32_t groups) { return rows / kMxTile + groups; }
@@ -611,11 +675,18 @@ int32_t describe(moe_handle *h, const char *who, int32_t rows, int32_t src_rows,
 
 using namespace moe;
 
+template <class E, bool kPair>
+static cudaError_t prepare_product()
+{
+    return cudaFuncSetAttribute(mxfp4_product_kernel<E, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pr_smem_bytes<kPair>());
+}
 cudaError_t moe::mxfp4_prepare()
 {
-    cudaError_t e = cudaFuncSetAttribute(mxfp4_product_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPrSmem);
-    if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(mxfp4_product_kernel<__half>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPrSmem);
+    cudaError_t e = prepare_product<__nv_bfloat16, false>();
+    if (e == cudaSuccess) e = prepare_product<__half, false>();
+    if (e == cudaSuccess) e = prepare_product<__nv_bfloat16, true>();
+    if (e == cudaSuccess) e = prepare_product<__half, true>();
+    return e;
 }
 
 extern "C" int32_t moe_mxfp4_scale_bytes(int32_t rows, int32_t K, int32_t groups, size_t *bytes)
@@ -686,17 +757,34 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     p.KQ = (K + kMxTile - 1) / kMxTile;
     p.num_kb = (K + kPrK - 1) / kPrK;
     p.last_steps = (K - (p.num_kb - 1) * kPrK + kPrStepK - 1) / kPrStepK;
-    p.NT = (N + kPrN - 1) / kPrN;
+    const bool pair = h->max_pairs > 0 && N > kPrN && rows / E_tot >= kPairRowsPerExpert;
+    const int32_t tile_n = pair ? PrCfg<true>::kTileN : PrCfg<false>::kTileN;
+    p.NT = (N + tile_n - 1) / tile_n;
     p.by_NT = divisor_of(p.NT);
     const int64_t used = rows < E_tot ? rows : E_tot, tiles = ((rows - used) / kPrRows + used) * p.NT;      // at most
     if (tiles >= (int64_t)1 << 31) return MOE_ERR_SHAPE;
-    if (!code_map(h, &p.tmW, w_codes, E_tot, N, K / 2, kPrN, "w_codes") || !code_map(h, &p.tmX[0], x_codes, 0, rows, K / 2, kPrRows, "x_codes") ||
-        !code_map(h, &p.tmX[1], x_codes, 0, rows, K / 2, 64, "x_codes") || !code_map(h, &p.tmX[2], x_codes, 0, rows, K / 2, 16, "x_codes") ||
+    const int32_t boxes[3] = {pair ? PrCfg<true>::kXRows : PrCfg<false>::kXRows, pair ? 32 : 64, 16};
+    for (int i = 0; i < (pair ? 2 : 3); ++i)
+        if (!code_map(h, &p.tmX[i], x_codes, 0, rows, K / 2, boxes[i], "x_codes")) return MOE_ERR_CUDA;
+    if (!code_map(h, &p.tmW, w_codes, E_tot, N, K / 2, kPrN, "w_codes") ||
         !scale_map(h, &p.tmXs, x_scales, scale_blocks(rows, E_tot), p.KQ, 2, "x_scales") ||
         !scale_map(h, &p.tmWs, w_scales, scale_blocks((int64_t)E_tot * N, E_tot), p.KQ, 1, "w_scales"))
         return MOE_ERR_CUDA;
-    const unsigned grid = (unsigned)(tiles < h->G ? tiles : h->G);
-    const cudaError_t err = launch_chained(dtype == MOE_BF16 ? mxfp4_product_kernel<__nv_bfloat16> : mxfp4_product_kernel<__half>, grid, kPrThreads, kPrSmem,
-                                           static_cast<cudaStream_t>(stream), p);
+    const int64_t slots = pair ? h->max_pairs : h->G, grid = tiles < slots ? tiles : slots;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2] = {chained_launch_attribute()};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pair ? 2 : 1;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cfg.gridDim = dim3((unsigned)(pair ? 2 * grid : grid));
+    cfg.blockDim = dim3(kPrThreads);
+    cfg.dynamicSmemBytes = pair ? pr_smem_bytes<true>() : pr_smem_bytes<false>();
+    const bool half = dtype == MOE_FP16;
+    const cudaError_t err = pair ? cudaLaunchKernelEx(&cfg, half ? mxfp4_product_kernel<__half, true> : mxfp4_product_kernel<__nv_bfloat16, true>, p)
+                                 : cudaLaunchKernelEx(&cfg, half ? mxfp4_product_kernel<__half, false> : mxfp4_product_kernel<__nv_bfloat16, false>, p);
     return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "grouped 4-bit product launch");
 }

@@ -446,6 +446,18 @@ def test_product_at_row_counts_around_the_steps(M):
     check_product(out, xv, wv, offsets, K, torch.bfloat16)
 
 
+@pytest.mark.parametrize("M", [1, 15, 17, 31, 32, 33, 63, 64, 65, 96, 97, 128, 129, 191, 192, 193, 256, 257, 320, 321, 385])
+@pytest.mark.parametrize("N, K", [(264, 384), (384, 1504)])
+def test_wide_tiles_at_row_counts_around_the_steps(M, N, K):
+    # many rows an expert on average: tiles of 256 columns by two CTAs
+    offsets = [0, 300, 300 + M, 700 + M]
+    xc, xs, wc, ws, xv, wv = product_case(offsets, 700 + M, N, K, M)
+    out, st = torch.empty((700 + M, N), dtype=torch.bfloat16, device="cuda"), status()
+    B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, ints(offsets), out, st)
+    assert st.tolist() == [0, 0, 0, 0]
+    check_product(out, xv, wv, offsets, K, torch.bfloat16)
+
+
 def test_product_with_exponents_far_apart():
     # exponents from far below to far above, every row and block another one: none is mixed up
     offsets, N, K = [0, 150, 300], 136, 512
