@@ -175,21 +175,21 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
 // TMEM holds two accumulators of 192 columns and, for five stages, 24 columns of exponents (128 rows of weights: 4 per 128
 // columns of K; 256 rows of x: 8; a pair's CTAs each have those of all rows of x); that is 504 of its 512 columns, and why a tile has
 // 192 rows and not 256.  A stage is 256 columns of K: 128 bytes of codes a row, a swizzle row.
-//   warps 0, 2  loaders (one thread each): codes of the weights, of the rows, and their exponents as they lie;
+//   warps 0, 2, 3, 12  loaders (one thread each): codes of the weights, of the rows, and the exponents of both as they lie;
 //   warp 1      copies the exponents to TMEM (tcgen05.cp, each of the four lane quarters gets them) and issues
 //               tcgen05.mma.kind::mxf4.block_scale (K = 64, two exponents a row); both are issued by one lane of the converged
 //               warp (pair: of the first CTA) and run in order;
 //   warps 4-11  epilogue: pieces of 32 rows x 32 columns, 16-bit, transposed in registers, 64 contiguous bytes a row.
 
-constexpr int kPrThreads = 384, kPrEpiWarps = 8;
+constexpr int kPrThreads = 416, kPrEpiWarps = 8;
 constexpr int kPrN = 128;                                   // output columns of a CTA's part of a tile (M of the MMA: a pair's twice that)
 constexpr int kPrRows = 192;                                // rows of a tile (N of the MMA)
 constexpr int kPrK = 256, kPrStepK = 64;                    // columns of K of a stage, of an MMA
 constexpr int kPrWBytes = kPrN * kPrK / 2;
 constexpr int kPrWScaleBytes = 2 * kMxTileBytes, kPrXScaleBytes = 4 * kMxTileBytes;      // x: row block 0 of both 128s of K, then row block 1
-constexpr int kPrScaleCols = 24, kPrScaleBuffers = 5;       // TMEM columns of a stage's exponents: weights 2 x 4, rows 2 x 8
+constexpr int kPrScaleCols = 24;                            // TMEM columns of a stage's exponents: weights 2 x 4, rows 2 x 8
 constexpr int kPrTmemCols = 512;
-constexpr int kPrMaxStages = 7;
+constexpr int kPrStages = 5;
 constexpr int kMaxExperts = 1024;
 template <bool kPair>
 struct PrCfg {
@@ -197,11 +197,11 @@ struct PrCfg {
     static constexpr int kXRows = kPair ? kPrRows / 2 : kPrRows;                         // rows of x that a CTA holds
     static constexpr int kXBytes = kXRows * kPrK / 2;
     static constexpr int kStageBytes = kPrWBytes + kXBytes + kPrWScaleBytes + kPrXScaleBytes;
-    static constexpr int kStages = kPair ? 7 : 5;
+    static constexpr int kStages = kPrStages;
     static constexpr int kRound = kPair ? 32 : 16;                                       // N of the MMA is a multiple of this
-    static_assert(kStageBytes % 1024 == 0 && kStages <= kPrMaxStages, "stages are 1024-byte aligned");
+    static_assert(kStageBytes % 1024 == 0, "stages are 1024-byte aligned");
 };
-static_assert(2 * kPrRows + kPrScaleBuffers * kPrScaleCols <= kPrTmemCols, "accumulators and exponents exceed TMEM");
+static_assert(2 * kPrRows + kPrStages * kPrScaleCols <= kPrTmemCols, "accumulators and exponents exceed TMEM");
 
 struct alignas(64) ProductParams {
     CUtensorMap tmW;               // codes [E][N][K / 2]   box 128 bytes x 128 rows, 128B swizzle
@@ -216,7 +216,7 @@ struct alignas(64) ProductParams {
     Divisor by_NT;
 };
 struct ProductControl {
-    unsigned long long full[kPrMaxStages], empty[kPrMaxStages], tmem_full[2], tmem_empty[2], drain;
+    unsigned long long full[kPrStages], empty[kPrStages], tmem_full[2], tmem_empty[2], drain;
     uint32_t tmem_base;
     volatile uint32_t abort;
     int32_t first[kMaxExperts + 1];       // row where an expert's rows begin
@@ -277,15 +277,15 @@ __device__ __forceinline__ uint32_t mxf4_idesc(uint32_t m, uint32_t n, uint32_t 
     return (2u * half << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24) | (2u * half << 29);
 }
 // Exponents, shared memory -> TMEM: 512 contiguous bytes are 32 rows of 16, which become 32 lanes x 4 columns in each of the four lane
-// quarters.  Descriptor: no swizzle, eights of rows 128 bytes apart (stride offset), version 1.
+// quarters.  Descriptor: no swizzle, eights of rows 128 bytes apart (stride offset), version 1; its low word is smem_desc_lo's.
 constexpr uint32_t kScaleDescHi = (128u >> 4) | (1u << 14);
-__device__ __forceinline__ uint32_t scale_desc_lo(uint32_t smem) { return ((smem & 0x3FFFFu) >> 4) | (1u << 16); }
-// One stage of operands in one statement: the exponents' copies (`two`: two row blocks of x), `steps` MMAs and the commit that hands the
+// One stage of operands in one statement: the exponents' copies (`two`: two row blocks of x), the MMAs and the commit that hands the
 // stage back, to both CTAs of a pair.  All of them are issued by one thread and run in order.  First the exponents of the first 128
-// columns, then of the second; 64 columns of codes are 32 bytes further along the swizzle row.
-#define MOE_MXF4_STAGE(GROUP, COMMIT) \
+// columns, then of the second; 64 columns of codes are 32 bytes further along the swizzle row.  AT1, AT2, AT3, T2: predicates
+// of the last stage, which may have fewer than four MMAs.
+#define MOE_MXF4_STAGE(GROUP, AT1, AT2, AT3, T2, COMMIT) \
     asm volatile( \
-        "{\n\t.reg .pred p, q, t, t1, s1, s2, s3;\n\t.reg .b64 da, db;\n\t.reg .b32 al, bl, sa, sb;\n\t" \
+        "{\n\t.reg .pred p, q, t, t1, s1, s2, s3;\n\t.reg .b64 da, db;\n\t.reg .b32 al, bl, sa, sb, sc;\n\t" \
         "setp.ne.b32 p, %11, 0;\n\t" \
         "setp.eq.b32 q, %11, %11;\n\t" \
         "setp.ne.b32 t, %8, 0;\n\t" \
@@ -293,51 +293,55 @@ __device__ __forceinline__ uint32_t scale_desc_lo(uint32_t smem) { return ((smem
         "setp.gt.u32 s2, %12, 2;\n\t" \
         "setp.gt.u32 s3, %12, 3;\n\t" \
         "and.pred t1, t, s2;\n\t" \
+        "add.u32 sa, %5, 4;\n\t" \
+        "add.u32 sb, %6, %7;\n\t" \
+        "add.u32 sc, sb, 8;\n\t" \
         "mov.b64 da, {%3, %15};\n\t" \
         "tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [%5], da;\n\t" \
         "mov.b64 da, {%4, %15};\n\t" \
         "tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [%6], da;\n\t" \
-        "add.u32 al, %4, 64;\n\tadd.u32 sa, %6, 4;\n\t" \
+        "add.u32 al, %4, 64;\n\tadd.u32 bl, %6, 4;\n\t" \
         "mov.b64 da, {al, %15};\n\t" \
-        "@t tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
-        "add.u32 al, %3, 32;\n\tadd.u32 sa, %5, 4;\n\t" \
+        "@t tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [bl], da;\n\t" \
+        "add.u32 al, %3, 32;\n\t" \
         "mov.b64 da, {al, %15};\n\t" \
-        "@s2 tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
-        "add.u32 al, %4, 32;\n\tadd.u32 sa, %6, 8;\n\t" \
+        AT2 "tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
+        "add.u32 al, %4, 32;\n\tadd.u32 bl, %6, 8;\n\t" \
         "mov.b64 da, {al, %15};\n\t" \
-        "@s2 tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
-        "add.u32 al, %4, 96;\n\tadd.u32 sa, %6, 12;\n\t" \
+        AT2 "tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [bl], da;\n\t" \
+        "add.u32 al, %4, 96;\n\tadd.u32 bl, %6, 12;\n\t" \
         "mov.b64 da, {al, %15};\n\t" \
-        "@t1 tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [sa], da;\n\t" \
-        "add.u32 sb, %6, %7;\n\t" \
+        T2 "tcgen05.cp.cta_group::" GROUP ".32x128b.warpx4 [bl], da;\n\t" \
         "mov.b64 da, {%1, %14};\n\tmov.b64 db, {%2, %14};\n\t" \
         "tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [%5], [sb], p;\n\t" \
         "add.u32 al, %1, 2;\n\tadd.u32 bl, %2, 2;\n\t" \
         "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t" \
-        "@s1 tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [%5], [sb], q;\n\t" \
-        "add.u32 sa, %5, 4;\n\tadd.u32 sb, sb, 8;\n\t" \
+        AT1 "tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [%5], [sb], q;\n\t" \
         "add.u32 al, %1, 4;\n\tadd.u32 bl, %2, 4;\n\t" \
         "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t" \
-        "@s2 tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [sa], [sb], q;\n\t" \
+        AT2 "tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %9, [sa], [sc], q;\n\t" \
         "add.u32 al, %1, 6;\n\tadd.u32 bl, %2, 6;\n\t" \
         "mov.b64 da, {al, %14};\n\tmov.b64 db, {bl, %14};\n\t" \
-        "@s3 tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [sa], [sb], q;\n\t" \
+        AT3 "tcgen05.mma.cta_group::" GROUP ".kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %10, [sa], [sc], q;\n\t" \
         COMMIT "\n\t}" \
         ::"r"(d_tmem), "r"(w_lo), "r"(x_lo), "r"(ws_lo), "r"(xs_lo), "r"(sw), "r"(sx), "r"(shift), "r"(two), "r"(idesc0), "r"(idesc1), "r"(accumulate), \
         "r"(steps), "r"(empty_bar), "r"(kSmemDescHi), "r"(kScaleDescHi), "h"((uint16_t)3) \
         : "memory")
-template <bool kPair>
+#define MOE_COMMIT_PAIR "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%13], %16;"
+#define MOE_COMMIT_ONE "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%13];"
+template <bool kPair, bool kWhole>
 __device__ __forceinline__ void tc_stage_mxf4(uint32_t d_tmem, uint32_t w_lo, uint32_t x_lo, uint32_t ws_lo, uint32_t xs_lo, uint32_t sw, uint32_t sx,
                                               uint32_t shift, uint32_t two, uint32_t idesc0, uint32_t idesc1, uint32_t accumulate, uint32_t steps,
                                               uint32_t empty_bar)
 {
-    if constexpr (kPair) {
-        MOE_MXF4_STAGE("2", "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%13], %16;");
-    } else {
-        MOE_MXF4_STAGE("1", "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%13];");
-    }
+    if constexpr (kPair && kWhole) MOE_MXF4_STAGE("2", "", "", "", "@t ", MOE_COMMIT_PAIR);
+    else if constexpr (kPair) MOE_MXF4_STAGE("2", "@s1 ", "@s2 ", "@s3 ", "@t1 ", MOE_COMMIT_PAIR);
+    else if constexpr (kWhole) MOE_MXF4_STAGE("1", "", "", "", "@t ", MOE_COMMIT_ONE);
+    else MOE_MXF4_STAGE("1", "@s1 ", "@s2 ", "@s3 ", "@t1 ", MOE_COMMIT_ONE);
 }
 #undef MOE_MXF4_STAGE
+#undef MOE_COMMIT_PAIR
+#undef MOE_COMMIT_ONE
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
 {
     asm volatile(
@@ -396,7 +400,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     const uint32_t rank = kPair ? cluster_ctarank() : 0u;
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::kStages; ++i) {
-            mbar_init(smem_u32(&ctl->full[i]), 2);            // the two loaders (pair: the first CTA's, which arm it for both)
+            mbar_init(smem_u32(&ctl->full[i]), 4);            // the four loaders (pair: the first CTA's, which arm it for both)
             mbar_init(smem_u32(&ctl->empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -457,63 +461,68 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     const unsigned long long deadline = globaltimer_ns() + P.wait_ns;
     ProductWalk<kPair> walk(P, ctl);
 
-    // Two loaders, one thread each, two copies a stage.  A tiled copy's issue takes its thread about 80 cycles whatever it brings, an
-    // untiled one 350: with one thread for the four tiled and three untiled copies that a stage once took (x in boxes of 64 rows, the
-    // exponents of every row block by themselves) the issue alone was 720 of a stage's 1100 cycles.  Pair: every copy completes on the
-    // first CTA's barrier, at the same offset there.
-    if (warp == 0) {
+    // Four loaders, one thread and one copy a stage each: codes of the weights, of the rows, and the exponents of both.  A tiled copy holds
+    // its thread up for about 260 cycles whatever it brings (an untiled one for longer): with two copies a thread the loads alone took 520
+    // cycles a stage, with one thread for the four tiled and three untiled copies that a stage once took (x in boxes of 64 rows, the
+    // exponents of every row block by themselves) 1100; the MMAs of a full stage take 400.  Pair: every copy completes on the first
+    // CTA's barrier, at the same offset there.
+    if (warp == 0 || warp == 2 || warp == 3 || warp == 4 + kPrEpiWarps) {
         if (lane == 0) {
             int stage = 0;
             uint32_t phase = 0, armed = 0;
             bool ok = true;
             for (; walk.g < total && ok; walk.next()) {
                 const ProductTile t = walk.tile(P, ctl);
-                const int n0 = t.n0 + (int)rank * kPrN, block = t.e * P.N / kMxTile + t.e + n0 / kMxTile;
-                for (int kb = 0; kb < P.num_kb; ++kb) {
+                // this loader's copy: map, where it goes in a stage, first coordinate and its step with the stages, the others
+                const CUtensorMap *map;
+                uint32_t at, bytes;
+                int x = 0, y, z = 0, dx = 0, dy = 0, boxes = 1;
+                if (warp == 0) {
+                    map = &P.tmW;
+                    at = 0u;
+                    bytes = kPrWBytes;
+                    dx = kPrK / 2;
+                    y = t.n0 + (int)rank * kPrN;
+                    z = t.e;
+                } else if (warp == 2) {
+                    // rows that this CTA holds of the tile: in one box, or in two of 64; those behind the tile's own are read for nothing
+                    const int held = kPair ? ((t.valid + C::kRound - 1) & -C::kRound) / 2 : t.valid;
+                    const int which = kPair ? (held > 32 ? 0 : 1) : held > 128 ? 0 : held > 16 ? 1 : 2;
+                    boxes = !kPair && which == 1 && held > 64 ? 2 : 1;
+                    map = &P.tmX[which];
+                    at = kPrWBytes;
+                    bytes = (which == 0 ? C::kXRows : which == 1 ? (kPair ? 32u : 64u) : 16u) * (kPrK / 2);
+                    dx = kPrK / 2;
+                    y = t.row0 + (int)rank * held;
+                } else if (warp == 3) {
+                    map = &P.tmWs;
+                    at = kPrWBytes + C::kXBytes;
+                    bytes = kPrWScaleBytes;
+                    y = 0;
+                    dy = 2;
+                    z = t.e * P.N / kMxTile + t.e + t.n0 / kMxTile + (int)rank;
+                } else {
+                    map = &P.tmXs;
+                    at = kPrWBytes + C::kXBytes + kPrWScaleBytes;
+                    bytes = kPrXScaleBytes;
+                    y = 0;
+                    dy = 2;
+                    // the row block that the quantisation put the tile's first row into: by the expert's first row (row0 - local)
+                    z = (t.row0 - t.local) / kMxTile + t.e + t.local / kMxTile;
+                }
+                for (int kb = 0; kb < P.num_kb; ++kb, x += dx, y += dy) {
                     ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 70u);
                     if (!ok) break;
-                    const uint32_t own = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * C::kStageBytes);
-                    if (rank == 0) mbar_arrive_expect_tx(own, (kPair ? 2u : 1u) * (uint32_t)(kPrWBytes + kPrWScaleBytes));
-                    if (kPair) {
-                        tma_load_3d_pair(dst, &P.tmW, own & 0xFEFFFFFFu, kb * (kPrK / 2), n0, t.e);
-                        tma_load_3d_pair(dst + kPrWBytes + C::kXBytes, &P.tmWs, own & 0xFEFFFFFFu, 0, 2 * kb, block);
+                    const uint32_t own = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * C::kStageBytes) + at;
+                    if (rank == 0) mbar_arrive_expect_tx(own, (kPair ? 2u : 1u) * (uint32_t)boxes * bytes);
+                    const uint32_t bar = kPair ? own & 0xFEFFFFFFu : own;
+                    if (warp == 2) {
+                        if (kPair) tma_load_2d_pair(dst, map, bar, x, y);
+                        else tma_load_2d(dst, map, bar, x, y);
+                        if (boxes == 2) tma_load_2d(dst + bytes, map, bar, x, y + 64);
                     } else {
-                        tma_load_3d(dst, &P.tmW, own, kb * (kPrK / 2), n0, t.e);
-                        tma_load_3d(dst + kPrWBytes + C::kXBytes, &P.tmWs, own, 0, 2 * kb, block);
-                    }
-                    armed |= 1u << stage;
-                    if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
-                }
-            }
-            if (!ok && rank == 0) pr_drain<C::kStages>(ctl, armed, stage, phase);
-        }
-        __syncwarp();
-    } else if (warp == 2) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0, armed = 0;
-            bool ok = true;
-            for (; walk.g < total && ok; walk.next()) {
-                const ProductTile t = walk.tile(P, ctl);
-                // rows that this CTA holds of the tile: in one box, or in two of 64; those behind the tile's own are read for nothing
-                const int held = kPair ? ((t.valid + C::kRound - 1) & -C::kRound) / 2 : t.valid, row0 = t.row0 + (int)rank * held;
-                const int which = kPair ? (held > 32 ? 0 : 1) : held > 128 ? 0 : held > 16 ? 1 : 2, boxes = !kPair && which == 1 && held > 64 ? 2 : 1;
-                const uint32_t box_bytes = (which == 0 ? C::kXRows : which == 1 ? (kPair ? 32u : 64u) : 16u) * (kPrK / 2);
-                const CUtensorMap *map = &P.tmX[which];
-                // the row block that the quantisation put the tile's first row into: by the expert's first row (row0 - local)
-                const int block = (t.row0 - t.local) / kMxTile + t.e + t.local / kMxTile;
-                for (int kb = 0; kb < P.num_kb; ++kb) {
-                    ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 74u);
-                    if (!ok) break;
-                    const uint32_t own = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * C::kStageBytes) + kPrWBytes;
-                    if (rank == 0) mbar_arrive_expect_tx(own, (kPair ? 2u : 1u) * ((uint32_t)boxes * box_bytes + kPrXScaleBytes));
-                    if (kPair) {
-                        tma_load_2d_pair(dst, map, own & 0xFEFFFFFFu, kb * (kPrK / 2), row0);
-                        tma_load_3d_pair(dst + C::kXBytes + kPrWScaleBytes, &P.tmXs, own & 0xFEFFFFFFu, 0, 2 * kb, block);
-                    } else {
-                        tma_load_2d(dst, map, own, kb * (kPrK / 2), row0);
-                        if (boxes == 2) tma_load_2d(dst + box_bytes, map, own, kb * (kPrK / 2), row0 + 64);
-                        tma_load_3d(dst + C::kXBytes + kPrWScaleBytes, &P.tmXs, own, 0, 2 * kb, block);
+                        if (kPair) tma_load_3d_pair(dst, map, bar, x, y, z);
+                        else tma_load_3d(dst, map, bar, x, y, z);
                     }
                     armed |= 1u << stage;
                     if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
@@ -523,51 +532,74 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         }
         __syncwarp();
     } else if (warp == 1 && rank == 0) {
-        // the whole warp runs the loop, converged, and one elected lane issues: warp-uniform operands (see the other products)
-        int stage = 0, it = 0, buffer = 0, early = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        const uint32_t ring0 = smem_u32(ring), lo0 = smem_desc_lo(ring0), sc0 = scale_desc_lo(ring0), full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
+        // The whole warp runs the loop, converged, and one elected lane issues: warp-uniform operands, addresses that advance by additions,
+        // the next stage's barrier looked at before this one's MMAs are issued.  The thread that issues paces the tensor pipe: with a
+        // wait that starts at the head of a stage, a second one for columns of exponents in shorter supply than stages, and addresses from
+        // the stage's number, it needed 450 cycles a stage without a single MMA; the MMAs take 400.
+        constexpr uint32_t kLoStage = (uint32_t)(C::kStageBytes >> 4), kLoX = (uint32_t)(kPrWBytes >> 4), kLoWs = (uint32_t)((kPrWBytes + C::kXBytes) >> 4),
+                           kLoXs = kLoWs + (uint32_t)(kPrWScaleBytes >> 4);
+        const uint32_t lo0 = smem_desc_lo(smem_u32(ring)), full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
+        const uint32_t sw0 = tmem_base + (uint32_t)(2 * kPrRows);
+        uint32_t w_lo = lo0, full_bar = full0, empty_bar = empty0, sw = sw0, phase = 0;
+        int it = 0;
+        bool ok = true, ready = mbar_test_wait(full0, 0u);
+        const auto wait_stage = [&]() {
+            if (__all_sync(0xffffffffu, ready)) return;
+            ok = __all_sync(0xffffffffu, pr_wait(full_bar, phase, ctl, deadline, P.status, (uint32_t)walk.g, 72u));
+        };
+        const auto advance = [&]() {
+            w_lo += kLoStage;
+            full_bar += 8u;
+            empty_bar += 8u;
+            sw += (uint32_t)kPrScaleCols;
+            if (full_bar == full0 + 8u * C::kStages) {
+                w_lo = lo0;
+                full_bar = full0;
+                empty_bar = empty0;
+                sw = sw0;
+                phase ^= 1u;
+            }
+        };
+        // the next stage's barrier, looked at early
+        const auto look = [&]() {
+            const bool wraps = full_bar == full0 + 8u * (C::kStages - 1);
+            ready = mbar_test_wait(wraps ? full0 : full_bar + 8u, wraps ? phase ^ 1u : phase);
+        };
         for (; walk.g < total && ok; walk.next(), ++it) {
             const ProductTile t = walk.tile(P, ctl);
             const int a = it & 1;
-            const uint32_t shift = (uint32_t)(t.local & (kMxTile - 1)) >> 5;                 // 0 or 2 columns: first row inside its row block
+            const uint32_t shift = __reduce_max_sync(0xffffffffu, (uint32_t)(t.local & (kMxTile - 1)) >> 5);     // 0 or 2 columns: first row inside its row block
             const uint32_t n = __reduce_max_sync(0xffffffffu, (uint32_t)((t.valid + C::kRound - 1) & -C::kRound)), two = 32u * shift + n > (uint32_t)kMxTile ? 1u : 0u;
             const uint32_t idesc0 = mxf4_idesc((uint32_t)C::kTileN, n, 0u), idesc1 = mxf4_idesc((uint32_t)C::kTileN, n, 1u);
-            ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), ((uint32_t)(it >> 1) & 1u) ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 71u));
+            const uint32_t parity = ((uint32_t)(it >> 1) & 1u) ^ 1u;
+            if (!__all_sync(0xffffffffu, mbar_test_wait(smem_u32(&ctl->tmem_empty[a]), parity))) {
+                ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), parity, ctl, deadline, P.status, (uint32_t)walk.g, 71u));
+                if (!ok) break;
+            }
+            const uint32_t d_tmem = tmem_base + (uint32_t)(a * kPrRows);
+            uint32_t accumulate = 0u;
+            for (int kb = 1; kb < P.num_kb; ++kb) {
+                wait_stage();
+                if (!ok) break;
+                tc_fence_after();
+                look();
+                if (elect_one_sync())
+                    tc_stage_mxf4<kPair, true>(d_tmem, w_lo, w_lo + kLoX, w_lo + kLoWs, w_lo + kLoXs, sw, sw + 8u, shift, two, idesc0, idesc1, accumulate, 4u, empty_bar);
+                accumulate = 1u;
+                advance();
+            }
+            if (!ok) break;
+            wait_stage();
             if (!ok) break;
             tc_fence_after();
-            const uint32_t d_tmem = tmem_base + (uint32_t)(a * kPrRows);
-            for (int kb = 0; kb < P.num_kb; ++kb) {
-                ok = __all_sync(0xffffffffu, pr_wait(full0 + 8u * stage, phase, ctl, deadline, P.status, (uint32_t)walk.g, 72u));
-                if (!ok) break;
-                if (C::kStages > kPrScaleBuffers) {
-                    // the exponents' columns are used again after fewer stages than the operands: the MMAs that read them last are done
-                    if (early < kPrScaleBuffers) {
-                        ++early;
-                    } else {
-                        const int then = stage >= kPrScaleBuffers ? stage - kPrScaleBuffers : stage + C::kStages - kPrScaleBuffers;
-                        const uint32_t parity = stage >= kPrScaleBuffers ? phase : phase ^ 1u;
-                        ok = __all_sync(0xffffffffu, pr_wait(empty0 + 8u * then, parity, ctl, deadline, P.status, (uint32_t)walk.g, 75u));
-                        if (!ok) break;
-                    }
-                }
-                tc_fence_after();
-                if (elect_one_sync()) {
-                    constexpr uint32_t kX = kPrWBytes >> 4, kWs = (kPrWBytes + C::kXBytes) >> 4, kXs = kWs + (kPrWScaleBytes >> 4);
-                    const uint32_t w_lo = lo0 + (uint32_t)(stage * (C::kStageBytes >> 4)), s_lo = sc0 + (uint32_t)(stage * (C::kStageBytes >> 4));
-                    const uint32_t sw = tmem_base + (uint32_t)(2 * kPrRows + buffer * kPrScaleCols);
-                    tc_stage_mxf4<kPair>(d_tmem, w_lo, w_lo + kX, s_lo + kWs, s_lo + kXs, sw, sw + 8u, shift, two, idesc0, idesc1, kb > 0 ? 1u : 0u,
-                                         kb == P.num_kb - 1 ? (uint32_t)P.last_steps : 4u, empty0 + 8u * stage);
-                    if (kb == P.num_kb - 1) {
-                        if (kPair) tc_commit_pair(smem_u32(&ctl->tmem_full[a]));
-                        else tc_commit(smem_u32(&ctl->tmem_full[a]));
-                    }
-                }
-                __syncwarp();
-                if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
-                if (++buffer == kPrScaleBuffers) buffer = 0;
+            look();
+            if (elect_one_sync()) {
+                tc_stage_mxf4<kPair, false>(d_tmem, w_lo, w_lo + kLoX, w_lo + kLoWs, w_lo + kLoXs, sw, sw + 8u, shift, two, idesc0, idesc1, accumulate,
+                                            (uint32_t)P.last_steps, empty_bar);
+                if (kPair) tc_commit_pair(smem_u32(&ctl->tmem_full[a]));
+                else tc_commit(smem_u32(&ctl->tmem_full[a]));
             }
+            advance();
         }
         if (!ok) {
             // what was issued finishes before shared memory and TMEM are released
@@ -580,7 +612,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < until) {}
         }
         __syncwarp();
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && warp < 4 + kPrEpiWarps) {
         const int q4 = warp & 3, grp = (warp - 4) >> 2;
         int it = 0;
         for (; walk.g < total; walk.next(), ++it) {
