@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
 // TMEM holds two accumulators of 192 columns and, for five stages, 24 columns of exponents (128 rows of weights: 4 per 128
 // columns of K; 256 rows of x: 8; a pair's CTAs each have those of all rows of x); that is 504 of its 512 columns, and why a tile has
 // 192 rows and not 256.  A stage is 256 columns of K: 128 bytes of codes a row, a swizzle row.
-//   warps 0, 2, 3, 12  loaders (one thread each): codes of the weights, of the rows, and the exponents of both as they lie;
+//   warps 0, 2, 3, 12  loaders: codes of the weights, of the rows, and the exponents of both as they lie;
 //   warp 1      copies the exponents to TMEM (tcgen05.cp, each of the four lane quarters gets them) and issues
 //               tcgen05.mma.kind::mxf4.block_scale (K = 64, two exponents a row); both are issued by one lane of the converged
 //               warp (pair: of the first CTA) and run in order;
@@ -377,16 +377,96 @@ __device__ __forceinline__ void store_piece(const uint32_t (&lo)[16], const uint
     }
 }
 
-// A loader's wind-down: the copies already issued land before shared memory is released
-template <int kStages>
-__device__ __forceinline__ void pr_drain(ProductControl *ctl, uint32_t armed, int stage, uint32_t phase)
+// A loader: one copy a stage, codes of the weights or of the rows, or the exponents of either.  The warp runs the loop converged and one
+// elected lane issues, as in the loop that issues the MMAs; operands advance by additions, the next stage's barrier is looked at early.  (One
+// thread, addresses worked out from the stage's number: 500 cycles a stage and copy, two copies 750, where the MMAs of a full stage
+// take 400; an untiled copy takes longer than a tiled one.)  Pair: every copy completes on the first CTA's barrier, at the same
+// offset there, and that CTA's loaders arm it for both.
+enum { kLoadW, kLoadX, kLoadWs, kLoadXs };
+template <bool kPair, int kWhat>
+__device__ __forceinline__ void product_loader(const ProductParams &P, ProductControl *ctl, ProductWalk<kPair> walk, int total, unsigned long long deadline,
+                                               uint32_t rank, uint8_t *ring)
 {
-    const unsigned long long drain = globaltimer_ns() + 2000000ull;
-    for (int i = 0; i < kStages; ++i) {
-        if (!(armed & (1u << i))) continue;
-        const uint32_t par = i < stage ? phase : (phase ^ 1u);
-        while (!mbar_try_wait(smem_u32(&ctl->full[i]), par) && globaltimer_ns() < drain) {}
+    using C = PrCfg<kPair>;
+    constexpr uint32_t kAt = kWhat == kLoadW ? 0 : kWhat == kLoadX ? kPrWBytes : kWhat == kLoadWs ? kPrWBytes + C::kXBytes : kPrWBytes + C::kXBytes + kPrWScaleBytes;
+    constexpr int kStep = kWhat == kLoadW || kWhat == kLoadX ? kPrK / 2 : 2;
+    const uint32_t dst0 = smem_u32(ring) + kAt, empty0 = smem_u32(&ctl->empty[0]), full0 = smem_u32(&ctl->full[0]);
+    uint32_t dst = dst0, empty_bar = empty0, full_bar = full0, phase = 0, armed = 0;
+    bool ok = true, ready = true;                              // (all stages are free at first)
+    for (; walk.g < total && ok; walk.next()) {
+        const ProductTile t = walk.tile(P, ctl);
+        const CUtensorMap *map;
+        int y, z = 0, boxes = 1;
+        uint32_t bytes;
+        if (kWhat == kLoadW) {
+            map = &P.tmW;
+            bytes = kPrWBytes;
+            y = t.n0 + (int)rank * kPrN;
+            z = t.e;
+        } else if (kWhat == kLoadX) {
+            // rows that this CTA holds of the tile: in one box, or in two of 64; those behind the tile's own are read for nothing
+            const int held = kPair ? ((t.valid + C::kRound - 1) & -C::kRound) / 2 : t.valid;
+            const int which = kPair ? (held > 32 ? 0 : 1) : held > 128 ? 0 : held > 16 ? 1 : 2;
+            boxes = !kPair && which == 1 && held > 64 ? 2 : 1;
+            map = &P.tmX[which];
+            bytes = (which == 0 ? C::kXRows : which == 1 ? (kPair ? 32u : 64u) : 16u) * (kPrK / 2);
+            y = t.row0 + (int)rank * held;
+        } else if (kWhat == kLoadWs) {
+            map = &P.tmWs;
+            bytes = kPrWScaleBytes;
+            y = t.e * P.N / kMxTile + t.e + t.n0 / kMxTile + (int)rank;
+        } else {
+            // the row block that the quantisation put the tile's first row into: by the expert's first row (row0 - local)
+            map = &P.tmXs;
+            bytes = kPrXScaleBytes;
+            y = (t.row0 - t.local) / kMxTile + t.e + t.local / kMxTile;
+        }
+        const uint32_t expected = (kPair ? 2u : 1u) * (uint32_t)boxes * bytes;
+        int x = 0;
+        for (int kb = 0; kb < P.num_kb; ++kb) {
+            if (!__all_sync(0xffffffffu, ready)) {
+                ok = __all_sync(0xffffffffu, pr_wait(empty_bar, phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 70u + kWhat));
+                if (!ok) break;
+            }
+            if (elect_one_sync()) {
+                if (!kPair || rank == 0) mbar_arrive_expect_tx(full_bar, expected);
+                const uint32_t bar = kPair ? full_bar & 0xFEFFFFFFu : full_bar;
+                if (kWhat == kLoadX) {
+                    if (kPair) tma_load_2d_pair(dst, map, bar, x, y);
+                    else tma_load_2d(dst, map, bar, x, y);
+                    if (!kPair && boxes == 2) tma_load_2d(dst + bytes, map, bar, x, y + 64);
+                } else if (kWhat == kLoadW) {
+                    if (kPair) tma_load_3d_pair(dst, map, bar, x, y, z);
+                    else tma_load_3d(dst, map, bar, x, y, z);
+                } else {
+                    if (kPair) tma_load_3d_pair(dst, map, bar, 0, x, y);
+                    else tma_load_3d(dst, map, bar, 0, x, y);
+                }
+            }
+            armed = min(armed + 1u, (uint32_t)C::kStages);
+            x += kStep;
+            dst += (uint32_t)C::kStageBytes;
+            empty_bar += 8u;
+            full_bar += 8u;
+            if (empty_bar == empty0 + 8u * C::kStages) {
+                dst = dst0;
+                empty_bar = empty0;
+                full_bar = full0;
+                phase ^= 1u;
+            }
+            ready = mbar_test_wait(empty_bar, phase ^ 1u);
+        }
     }
+    if (!ok && rank == 0) {
+        // wind-down: the copies already issued land before shared memory is released
+        const int stage = (int)(empty_bar - empty0) >> 3;
+        const unsigned long long drain = globaltimer_ns() + 2000000ull;
+        for (int i = 0; i < C::kStages; ++i) {
+            if (i >= stage && armed < (uint32_t)C::kStages) continue;
+            while (!mbar_try_wait(smem_u32(&ctl->full[i]), i < stage ? phase : phase ^ 1u) && globaltimer_ns() < drain) {}
+        }
+    }
+    __syncwarp();
 }
 
 template <class E, bool kPair>
@@ -461,77 +541,11 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     const unsigned long long deadline = globaltimer_ns() + P.wait_ns;
     ProductWalk<kPair> walk(P, ctl);
 
-    // Four loaders, one thread and one copy a stage each: codes of the weights, of the rows, and the exponents of both.  A tiled copy holds
-    // its thread up for about 260 cycles whatever it brings (an untiled one for longer): with two copies a thread the loads alone took 520
-    // cycles a stage, with one thread for the four tiled and three untiled copies that a stage once took (x in boxes of 64 rows, the
-    // exponents of every row block by themselves) 1100; the MMAs of a full stage take 400.  Pair: every copy completes on the first
-    // CTA's barrier, at the same offset there.
-    if (warp == 0 || warp == 2 || warp == 3 || warp == 4 + kPrEpiWarps) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0, armed = 0;
-            bool ok = true;
-            for (; walk.g < total && ok; walk.next()) {
-                const ProductTile t = walk.tile(P, ctl);
-                // this loader's copy: map, where it goes in a stage, first coordinate and its step with the stages, the others
-                const CUtensorMap *map;
-                uint32_t at, bytes;
-                int x = 0, y, z = 0, dx = 0, dy = 0, boxes = 1;
-                if (warp == 0) {
-                    map = &P.tmW;
-                    at = 0u;
-                    bytes = kPrWBytes;
-                    dx = kPrK / 2;
-                    y = t.n0 + (int)rank * kPrN;
-                    z = t.e;
-                } else if (warp == 2) {
-                    // rows that this CTA holds of the tile: in one box, or in two of 64; those behind the tile's own are read for nothing
-                    const int held = kPair ? ((t.valid + C::kRound - 1) & -C::kRound) / 2 : t.valid;
-                    const int which = kPair ? (held > 32 ? 0 : 1) : held > 128 ? 0 : held > 16 ? 1 : 2;
-                    boxes = !kPair && which == 1 && held > 64 ? 2 : 1;
-                    map = &P.tmX[which];
-                    at = kPrWBytes;
-                    bytes = (which == 0 ? C::kXRows : which == 1 ? (kPair ? 32u : 64u) : 16u) * (kPrK / 2);
-                    dx = kPrK / 2;
-                    y = t.row0 + (int)rank * held;
-                } else if (warp == 3) {
-                    map = &P.tmWs;
-                    at = kPrWBytes + C::kXBytes;
-                    bytes = kPrWScaleBytes;
-                    y = 0;
-                    dy = 2;
-                    z = t.e * P.N / kMxTile + t.e + t.n0 / kMxTile + (int)rank;
-                } else {
-                    map = &P.tmXs;
-                    at = kPrWBytes + C::kXBytes + kPrWScaleBytes;
-                    bytes = kPrXScaleBytes;
-                    y = 0;
-                    dy = 2;
-                    // the row block that the quantisation put the tile's first row into: by the expert's first row (row0 - local)
-                    z = (t.row0 - t.local) / kMxTile + t.e + t.local / kMxTile;
-                }
-                for (int kb = 0; kb < P.num_kb; ++kb, x += dx, y += dy) {
-                    ok = pr_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, ctl, deadline, P.status, (uint32_t)walk.g, 70u);
-                    if (!ok) break;
-                    const uint32_t own = smem_u32(&ctl->full[stage]), dst = smem_u32(ring + stage * C::kStageBytes) + at;
-                    if (rank == 0) mbar_arrive_expect_tx(own, (kPair ? 2u : 1u) * (uint32_t)boxes * bytes);
-                    const uint32_t bar = kPair ? own & 0xFEFFFFFFu : own;
-                    if (warp == 2) {
-                        if (kPair) tma_load_2d_pair(dst, map, bar, x, y);
-                        else tma_load_2d(dst, map, bar, x, y);
-                        if (boxes == 2) tma_load_2d(dst + bytes, map, bar, x, y + 64);
-                    } else {
-                        if (kPair) tma_load_3d_pair(dst, map, bar, x, y, z);
-                        else tma_load_3d(dst, map, bar, x, y, z);
-                    }
-                    armed |= 1u << stage;
-                    if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
-                }
-            }
-            if (!ok && rank == 0) pr_drain<C::kStages>(ctl, armed, stage, phase);
-        }
-        __syncwarp();
-    } else if (warp == 1 && rank == 0) {
+    if (warp == 0) product_loader<kPair, kLoadW>(P, ctl, walk, total, deadline, rank, ring);
+    else if (warp == 2) product_loader<kPair, kLoadX>(P, ctl, walk, total, deadline, rank, ring);
+    else if (warp == 3) product_loader<kPair, kLoadWs>(P, ctl, walk, total, deadline, rank, ring);
+    else if (warp == 4 + kPrEpiWarps) product_loader<kPair, kLoadXs>(P, ctl, walk, total, deadline, rank, ring);
+    else if (warp == 1 && rank == 0) {
         // The whole warp runs the loop, converged, and one elected lane issues: warp-uniform operands, addresses that advance by additions,
         // the next stage's barrier looked at before this one's MMAs are issued.  The thread that issues paces the tensor pipe: with a
         // wait that starts at the head of a stage, a second one for columns of exponents in shorter supply than stages, and addresses from
@@ -545,7 +559,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         bool ok = true, ready = mbar_test_wait(full0, 0u);
         const auto wait_stage = [&]() {
             if (__all_sync(0xffffffffu, ready)) return;
-            ok = __all_sync(0xffffffffu, pr_wait(full_bar, phase, ctl, deadline, P.status, (uint32_t)walk.g, 72u));
+            ok = __all_sync(0xffffffffu, pr_wait(full_bar, phase, ctl, deadline, P.status, (uint32_t)walk.g, 76u));
         };
         const auto advance = [&]() {
             w_lo += kLoStage;
@@ -573,7 +587,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             const uint32_t idesc0 = mxf4_idesc((uint32_t)C::kTileN, n, 0u), idesc1 = mxf4_idesc((uint32_t)C::kTileN, n, 1u);
             const uint32_t parity = ((uint32_t)(it >> 1) & 1u) ^ 1u;
             if (!__all_sync(0xffffffffu, mbar_test_wait(smem_u32(&ctl->tmem_empty[a]), parity))) {
-                ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), parity, ctl, deadline, P.status, (uint32_t)walk.g, 71u));
+                ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), parity, ctl, deadline, P.status, (uint32_t)walk.g, 75u));
                 if (!ok) break;
             }
             const uint32_t d_tmem = tmem_base + (uint32_t)(a * kPrRows);
@@ -619,7 +633,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             const ProductTile t = walk.tile(P, ctl);
             const int a = it & 1, pieces = (t.valid + 31) >> 5, col = t.n0 + (int)rank * kPrN + q4 * 32, cols = P.N - col;
             uint32_t ok = 1u;
-            if (lane == 0) ok = pr_wait(smem_u32(&ctl->tmem_full[a]), (uint32_t)(it >> 1) & 1u, ctl, deadline, P.status, (uint32_t)walk.g, 73u) ? 1u : 0u;
+            if (lane == 0) ok = pr_wait(smem_u32(&ctl->tmem_full[a]), (uint32_t)(it >> 1) & 1u, ctl, deadline, P.status, (uint32_t)walk.g, 77u) ? 1u : 0u;
             if (!__shfl_sync(0xffffffffu, ok, 0)) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(a * kPrRows);
