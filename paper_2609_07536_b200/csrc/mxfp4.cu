@@ -219,6 +219,7 @@ struct ProductControl {
     unsigned long long full[kPrStages], empty[kPrStages], tmem_full[2], tmem_empty[2], drain;
     uint32_t tmem_base;
     volatile uint32_t abort;
+    int32_t warp_tiles[kPrThreads / 32];
     int32_t first[kMaxExperts + 1];       // row where an expert's rows begin
     int32_t tiles[kMaxExperts + 1];       // row tiles of the experts before
 };
@@ -469,6 +470,37 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
     __syncwarp();
 }
 
+// The same by one warp, whatever the offsets and however many: a running maximum, clamped to the rows
+__device__ __noinline__ void repair_offsets(const ProductParams &P, ProductControl *ctl, int lane)
+{
+    int tiles = 0, before = 0;
+    for (int e0 = 0; e0 <= P.E; e0 += 32) {
+        const int e = e0 + lane, raw = ctl->first[min(e, P.E)];
+        int o = min(max(raw, before), P.R);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, o, d);
+            if (lane >= d) o = max(o, u);
+        }
+        if (e <= P.E && o != raw && blockIdx.x == 0) report(P.status, MOE_DEV_OOB, (uint32_t)e, 63u);
+        int prev = __shfl_up_sync(0xffffffffu, o, 1);
+        if (lane == 0) prev = before;
+        // row tiles of the expert that ends at `o` (expert e - 1)
+        int t = (e > 0 && e <= P.E) ? (o - prev + kPrRows - 1) / kPrRows : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, t, d);
+            if (lane >= d) t += u;
+        }
+        if (e <= P.E) {
+            ctl->first[e] = o;
+            ctl->tiles[e] = tiles + t;
+        }
+        before = __shfl_sync(0xffffffffu, o, 31);
+        tiles += __shfl_sync(0xffffffffu, t, 31);
+    }
+}
+
 template <class E, bool kPair>
 __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __grid_constant__ ProductParams P)
 {
@@ -501,38 +533,36 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         else tmem_alloc(smem_u32(&ctl->tmem_base), kPrTmemCols);
     }
     grid_dependency_wait();
-    for (int e = threadIdx.x; e <= P.E; e += kPrThreads) ctl->first[e] = ld_chained(P.offsets + e);
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    if (warp == 3) {
-        // where the experts' rows begin and how many row tiles lie before them; what is out of range is reported and has no rows
-        int tiles = 0, before = 0;
-        for (int e0 = 0; e0 <= P.E; e0 += 32) {
-            const int e = e0 + lane, raw = ctl->first[min(e, P.E)];
-            int o = min(max(raw, before), P.R);
+    // Where the experts' rows begin and how many row tiles lie before them.  A thread has an expert; offsets that go back or past the rows
+    // are reported, and what they name has no rows.
+    if (P.E <= kPrThreads - 1) {
+        const int e = (int)threadIdx.x;
+        const int o = ld_chained(P.offsets + min(e, P.E)), next = ld_chained(P.offsets + min(e + 1, P.E));
+        int t = e < P.E ? (next - o + kPrRows - 1) / kPrRows : 0;
+        const int own = t;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {                     // running maximum: offsets never go back
-                const int u = __shfl_up_sync(0xffffffffu, o, d);
-                if (lane >= d) o = max(o, u);
-            }
-            if (e <= P.E && o != raw && blockIdx.x == 0) report(P.status, MOE_DEV_OOB, (uint32_t)e, 63u);
-            int prev = __shfl_up_sync(0xffffffffu, o, 1);
-            if (lane == 0) prev = before;
-            // row tiles of the expert that ends at `o` (expert e - 1)
-            int t = (e > 0 && e <= P.E) ? (o - prev + kPrRows - 1) / kPrRows : 0;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int u = __shfl_up_sync(0xffffffffu, t, d);
-                if (lane >= d) t += u;
-            }
-            if (e <= P.E) {
-                ctl->first[e] = o;
-                ctl->tiles[e] = tiles + t;
-            }
-            before = __shfl_sync(0xffffffffu, o, 31);
-            tiles += __shfl_sync(0xffffffffu, t, 31);
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, t, d);
+            if (lane >= d) t += u;
         }
+        if (e <= P.E) ctl->first[e] = o;
+        if (lane == 31) ctl->warp_tiles[warp] = t;
+        tc_fence_before();
+        const bool fine = __syncthreads_and(o >= 0 && o <= next && next <= P.R) != 0;
+        tc_fence_after();
+        if (fine) {
+            int base = 0;
+            for (int w = 0; w < warp; ++w) base += ctl->warp_tiles[w];
+            if (e <= P.E) ctl->tiles[e] = base + t - own;
+        } else if (warp == 3) {
+            repair_offsets(P, ctl, lane);
+        }
+    } else {
+        for (int e = threadIdx.x; e <= P.E; e += kPrThreads) ctl->first[e] = ld_chained(P.offsets + e);
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        if (warp == 3) repair_offsets(P, ctl, lane);
     }
     __syncthreads();
     if (kPair) cluster_sync_all();     // the other CTA's barriers exist before anything arrives on them
