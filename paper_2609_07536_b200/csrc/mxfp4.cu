@@ -705,7 +705,12 @@ template <bool kPair>
 constexpr size_t pr_smem_bytes() { return (size_t)PrCfg<kPair>::kStages * PrCfg<kPair>::kStageBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127); }
 static_assert(pr_smem_bytes<false>() <= 227 * 1024 && pr_smem_bytes<true>() <= 227 * 1024, "the product's stages exceed the shared memory of an SM");
 
-constexpr int32_t kPairRowsPerExpert = 64;
+// Mean rows per expert from which tiles by pairs of CTAs pay: they read less per product, but there are half as many places for them.
+// One CTA / pair, us, skewed routing, at 80 / 136 / 181 to 200 / 248 to 300 / 409 to 546 / 992 or more rows per expert:
+//   N 2816, K 2048   44.5/45.1  44.3/44.1  58.3/56.7  70.2/66.7  118/109  214/196
+//   N 2048, K 1408   28.7/28.9  29.6/29.6  35.6/35.1  43.1/41.6  73.2/66.0  134/120
+//   N 1024, K 1536   12.4/13.4  14.5/15.3  17.5/18.5  19.8/20.5  22.8/22.7  62.8/59.8
+constexpr int32_t kPairRowsPerExpert = 256;
 
 bool columns_ok(int32_t K) { return K >= kMxBlock && K % kMxBlock == 0 && K <= 1 << 20; }
 int64_t scale_blocks(int64_t rows, int32_t groups) { return rows / kMxTile + groups; }

@@ -416,7 +416,7 @@ def check_product(out, xv, wv, offsets, K, dtype):
 
 PRODUCTS = [
     ([0, 1], 1, 8, 32), ([0, 1], 1, 128, 256), ([0, 3, 3, 4], 4, 24, 64), ([0, 16, 33], 40, 136, 96), ([0, 64, 64, 129], 129, 256, 160),
-    ([0, 191, 383, 576], 576, 128, 256), ([0, 193, 193, 600], 640, 264, 288), ([0, 400, 1003], 1003, 1408, 512), ([0, 0, 0, 7], 7, 2048, 1408),
+    ([0, 191, 383, 576], 576, 128, 256), ([0, 193, 193, 600], 640, 264, 288), ([0, 193, 193, 700], 800, 264, 288), ([0, 400, 1003], 1003, 1408, 512), ([0, 0, 0, 7], 7, 2048, 1408),
     ([0] + list(range(1, 67)), 66, 384, 1280),
 ]
 
@@ -450,40 +450,54 @@ def test_product_at_row_counts_around_the_steps(M):
 @pytest.mark.parametrize("N, K", [(264, 384), (384, 1504)])
 def test_wide_tiles_at_row_counts_around_the_steps(M, N, K):
     # many rows an expert on average: tiles of 256 columns by two CTAs
-    offsets = [0, 300, 300 + M, 700 + M]
-    xc, xs, wc, ws, xv, wv = product_case(offsets, 700 + M, N, K, M)
-    out, st = torch.empty((700 + M, N), dtype=torch.bfloat16, device="cuda"), status()
+    offsets = [0, 300, 300 + M, 800 + M]
+    xc, xs, wc, ws, xv, wv = product_case(offsets, 800 + M, N, K, M)
+    out, st = torch.empty((800 + M, N), dtype=torch.bfloat16, device="cuda"), status()
     B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, ints(offsets), out, st)
     assert st.tolist() == [0, 0, 0, 0]
     check_product(out, xv, wv, offsets, K, torch.bfloat16)
 
 
-def test_product_with_exponents_far_apart():
+@pytest.mark.parametrize("offsets, rows", [([0, 150, 300], 300), ([0, 250, 600], 600)])
+def test_product_with_exponents_far_apart(offsets, rows):
     # exponents from far below to far above, every row and block another one: none is mixed up
-    offsets, N, K = [0, 150, 300], 136, 512
-    E = 2
-    ex = torch.randint(-30, 30, (300, K // 32, 1), generator=gen(1)).float()
-    x = (normal((300, K // 32, 32), torch.float32, 2) * torch.exp2(ex)).reshape(300, K)
+    N, K, E = 136, 512, 2
+    ex = torch.randint(-30, 30, (rows, K // 32, 1), generator=gen(1)).float()
+    x = (normal((rows, K // 32, 32), torch.float32, 2) * torch.exp2(ex)).reshape(rows, K)
     ew = torch.randint(-30, 30, (E * N, K // 32, 1), generator=gen(3)).float()
     w = (normal((E * N, K // 32, 32), torch.float32, 4) * torch.exp2(ew)).reshape(E * N, K)
     xc, xs, _ = quantized(x.cuda(), E, ints(offsets))
     wc, ws, _ = quantized(w.cuda(), E)
-    out, st = torch.empty((300, N), dtype=torch.bfloat16, device="cuda"), status()
+    out, st = torch.empty((rows, N), dtype=torch.bfloat16, device="cuda"), status()
     B.moe_mxfp4_gemm(handle(), xc, xs, wc.reshape(E, N, K // 2), ws, ints(offsets), out, st)
     check_product(out, ref.dequantize(*ref.quantize(f64(x))), ref.dequantize(*ref.quantize(f64(w))).reshape(E, N, K), offsets, K, torch.bfloat16)
 
 
-def test_no_number_in_a_product_stays_in_its_row_and_column():
-    offsets, N, K = [0, 70, 200], 136, 256
-    x, w = normal((200, K), torch.float32, 1), normal((2 * N, K), torch.float32, 2)
+@pytest.mark.parametrize("far", [0, 500])
+def test_no_number_in_a_product_stays_in_its_row_and_column(far):
+    rows = 200 + far                                    # (few rows an expert, many)
+    offsets, N, K = [0, 70, rows], 136, 256
+    x, w = normal((rows, K), torch.float32, 1), normal((2 * N, K), torch.float32, 2)
     x[90, 40] = float("nan")                            # expert 1
     w[5, 200] = float("inf")                            # expert 0, column 5
     xc, xs, _ = quantized(x.cuda(), 2, ints(offsets))
     wc, ws, _ = quantized(w.cuda(), 2)
-    out, st = torch.empty((200, N), dtype=torch.bfloat16, device="cuda"), status()
+    out, st = torch.empty((rows, N), dtype=torch.bfloat16, device="cuda"), status()
     B.moe_mxfp4_gemm(handle(), xc, xs, wc.reshape(2, N, K // 2), ws, ints(offsets), out, st)
     bad = np.isnan(f64(out))
     assert bad[90].all() and bad[:70, 5].all() and bad.sum() == N + 70
+
+
+def test_more_experts_than_threads():
+    E, N, K = 1000, 16, 64
+    counts = np.random.default_rng(0).integers(0, 4, size=E)
+    offsets = [0] + np.cumsum(counts).tolist()
+    xc, xs, wc, ws, xv, wv = product_case(offsets, offsets[-1] + 3, N, K, 3)
+    out, st = torch.full((offsets[-1] + 3, N), 7.0, dtype=torch.bfloat16, device="cuda"), status()
+    B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, ints(offsets), out, st)
+    assert st.tolist() == [0, 0, 0, 0]
+    check_product(out, xv, wv, offsets, K, torch.bfloat16)
+    assert (f64(out)[offsets[-1]:] == 7.0).all()
 
 
 def test_product_reports_offsets_that_go_back():
