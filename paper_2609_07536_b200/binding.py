@@ -431,15 +431,19 @@ _i32 = _u8 = _f32 = None
 _current_raw_stream = None
 
 
-def _device():
-    """The calling thread's current CUDA device (the first call fills the tables of element types)."""
+def _first_look():
+    """Fills the tables of element types and looks up torch's own ways to the current device and stream."""
+    global _i32, _u8, _f32, _current_raw_stream, _device
     import torch
-    if not _types:
-        global _i32, _u8, _f32, _current_raw_stream
-        _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        _i32, _u8, _f32 = torch.int32, torch.uint8, torch.float32
-        _types.update({torch.bfloat16: MOE_BF16, torch.float16: MOE_FP16, torch.float32: MOE_FP32})
-    return torch.cuda.current_device()
+    now = torch.cuda.current_device()
+    _i32, _u8, _f32 = torch.int32, torch.uint8, torch.float32
+    _types.update({torch.bfloat16: MOE_BF16, torch.float16: MOE_FP16, torch.float32: MOE_FP32})
+    _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # (the public call checks that CUDA is up every time)
+    return now
+
+
+_device = _first_look        # the calling thread's current CUDA device
 
 
 def _row_type(kind, who):
@@ -452,7 +456,7 @@ def _row_type(kind, who):
 def _matrix(t, rows, cols, kind, device, who, what):
     """(address, row distance) of a matrix of at least `rows` x exactly `cols` with contiguous columns."""
     shape = t.shape
-    if len(shape) == 2 and shape[0] >= rows and shape[1] == cols and t.dtype is kind and t.get_device() == device:
+    if t.dtype is kind and len(shape) == 2 and shape[1] == cols and shape[0] >= rows and t.get_device() == device:
         if t.is_contiguous():
             return t.data_ptr(), cols
         ld, one = t.stride()
@@ -493,7 +497,7 @@ def moe_permute(h, tokens, inv_perm, shape, rows, status_dev, stream=None):
     a, lda = _matrix(tokens, shape.T, shape.H, tokens.dtype, dev, who, "tokens")
     b, ldb = _matrix(rows, R, shape.H, tokens.dtype, dev, who, "rows")
     _check((_lib or lib()).moe_permute(h, a, lda, _vector(inv_perm, R, _i32, dev, who, "inv_perm"), C.byref(shape), _row_type(tokens.dtype, who), b, ldb,
-                             _ptr(status_dev), _raw_stream(stream, dev)), who, h)
+                             _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
 
 
 def moe_permute_grad(h, d_rows, inv_perm, shape, d_tokens, status_dev, stream=None):
@@ -502,7 +506,7 @@ def moe_permute_grad(h, d_rows, inv_perm, shape, d_tokens, status_dev, stream=No
     a, lda = _matrix(d_rows, R, shape.H, d_rows.dtype, dev, who, "d_rows")
     b, ldb = _matrix(d_tokens, shape.T, shape.H, d_rows.dtype, dev, who, "d_tokens")
     _check((_lib or lib()).moe_permute_grad(h, a, lda, _vector(inv_perm, R, _i32, dev, who, "inv_perm"), C.byref(shape), _row_type(d_rows.dtype, who), b, ldb,
-                                  _ptr(status_dev), _raw_stream(stream, dev)), who, h)
+                                  _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
 
 
 def moe_unpermute(h, rows, inv_perm, topk_w, shape, out, status_dev, stream=None):
@@ -512,7 +516,7 @@ def moe_unpermute(h, rows, inv_perm, topk_w, shape, out, status_dev, stream=None
     b, ldb = _matrix(out, shape.T, shape.H, rows.dtype, dev, who, "out")
     _check((_lib or lib()).moe_unpermute(h, a, lda, _vector(inv_perm, R, _i32, dev, who, "inv_perm"),
                                _vector(topk_w, R, _f32, dev, who, "topk_w"), C.byref(shape), _row_type(rows.dtype, who), b, ldb,
-                               _ptr(status_dev), _raw_stream(stream, dev)), who, h)
+                               _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
 
 
 def moe_unpermute_grad(h, d_out, rows, inv_perm, topk_w, shape, d_rows, d_topk_w, status_dev, stream=None):
@@ -523,7 +527,7 @@ def moe_unpermute_grad(h, d_out, rows, inv_perm, topk_w, shape, d_rows, d_topk_w
     c, ldc = _matrix(d_rows, R, shape.H, d_out.dtype, dev, who, "d_rows")
     _check((_lib or lib()).moe_unpermute_grad(h, a, lda, b, ldb, _vector(inv_perm, R, _i32, dev, who, "inv_perm"),
                                     _vector(topk_w, R, _f32, dev, who, "topk_w"), C.byref(shape), _row_type(d_out.dtype, who), c, ldc,
-                                    _vector(d_topk_w, R, _f32, dev, who, "d_topk_w"), _ptr(status_dev), _raw_stream(stream, dev)), who, h)
+                                    _vector(d_topk_w, R, _f32, dev, who, "d_topk_w"), _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
 
 
 def moe_gated_act(h, gate_up, act, codes=None, scales=None, stream=None):
@@ -573,7 +577,7 @@ def moe_mxfp4_quantize(h, src, codes, scales, groups, status_dev, offsets=None, 
         raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm names {inv_perm.numel()} rows, codes have {rows}")
     a, lda = _matrix(src, rows // max(1, copies), K, src.dtype, dev, who, "src")
     _check((_lib or lib()).moe_mxfp4_quantize(h, a, lda, _row_type(src.dtype, who), rows, K, groups, _vector(offsets, groups + 1, _i32, dev, who, "offsets"),
-                                    _vector(inv_perm, rows, _i32, dev, who, "inv_perm"), copies, c, sc, _ptr(status_dev), _raw_stream(stream, dev)), who, h)
+                                    _vector(inv_perm, rows, _i32, dev, who, "inv_perm"), copies, c, sc, _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
 
 
 def moe_mxfp4_dequantize(h, codes, scales, groups, out, status_dev, offsets=None, stream=None):
@@ -582,7 +586,7 @@ def moe_mxfp4_dequantize(h, codes, scales, groups, out, status_dev, offsets=None
     c, sc, rows, K = _mxfp4_operand(codes, scales, groups, dev, who)
     a, lda = _matrix(out, rows, K, out.dtype, dev, who, "out")
     _check((_lib or lib()).moe_mxfp4_dequantize(h, c, sc, rows, K, groups, _vector(offsets, groups + 1, _i32, dev, who, "offsets"), _row_type(out.dtype, who),
-                                      a, lda, _ptr(status_dev), _raw_stream(stream, dev)), who, h)
+                                      a, lda, _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
 
 
 def moe_mxfp4_gemm(h, x_codes, x_scales, w_codes, w_scales, offsets, out, status_dev, stream=None):
@@ -597,7 +601,7 @@ def moe_mxfp4_gemm(h, x_codes, x_scales, w_codes, w_scales, offsets, out, status
         raise MoeError(MOE_ERR_SHAPE, who, f"x has {K} columns, w {Kw}")
     a, lda = _matrix(out, rows, N, out.dtype, dev, who, "out")
     _check((_lib or lib()).moe_mxfp4_gemm(h, x, xs, w, ws, _vector(offsets, E + 1, _i32, dev, who, "offsets"), rows, E, N, K, _row_type(out.dtype, who), a, lda,
-                                _ptr(status_dev), _raw_stream(stream, dev)), who, h)
+                                _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
 
 
 # ----------------------------------------------------------------------------- device memory plumbing

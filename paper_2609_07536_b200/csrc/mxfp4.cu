@@ -550,11 +550,11 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         tc_fence_before();
         const bool fine = __syncthreads_and(o >= 0 && o <= next && next <= P.R) != 0;
         tc_fence_after();
-        if (fine) {
+        if (fine && 32 * warp <= P.E) {
             int base = 0;
             for (int w = 0; w < warp; ++w) base += ctl->warp_tiles[w];
             if (e <= P.E) ctl->tiles[e] = base + t - own;
-        } else if (warp == 3) {
+        } else if (!fine && warp == 3) {
             repair_offsets(P, ctl, lane);
         }
     } else {
