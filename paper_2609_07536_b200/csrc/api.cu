@@ -90,6 +90,13 @@ bool code_map(moe_handle *h, CUtensorMap *map, const void *ptr, int32_t planes, 
     return encode_map(h, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, ptr, planes ? 3 : 2, dims, strides, box, name);
 }
 
+bool out_map(moe_handle *h, CUtensorMap *map, const void *ptr, int64_t rows, int32_t cols, int64_t ld, int32_t box_cols, int32_t box_rows, const char *name)
+{
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    return encode_map(h, map, CU_TENSOR_MAP_DATA_TYPE_UINT16, ptr, 2, dims, strides, box, name);
+}
+
 bool scale_map(moe_handle *h, CUtensorMap *map, const void *ptr, int64_t row_blocks, int32_t col_blocks, int32_t box_blocks, const char *name)
 {
     // a block's 512 bytes as 128 words: a box has at most 256 elements a side

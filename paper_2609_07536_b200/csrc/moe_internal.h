@@ -269,6 +269,8 @@ const CUtensorMap *operand_map(moe_handle *h, const void *ptr, int32_t planes, i
 const CUtensorMap *gate_up_map(moe_handle *h, const void *ptr, int32_t experts, int32_t inter, int32_t cols, int32_t box_inter, const char *name);
 // ... of rows of bytes (planes = 0: two dimensions), boxes of 128 bytes x box_rows, 128B swizzle; encoded anew by every call
 bool code_map(moe_handle *h, CUtensorMap *map, const void *ptr, int32_t planes, int64_t rows, int32_t row_bytes, int32_t box_rows, const char *name);
+// ... of 16-bit rows with `ld` elements between them, boxes of box_cols x box_rows, 128B swizzle
+bool out_map(moe_handle *h, CUtensorMap *map, const void *ptr, int64_t rows, int32_t cols, int64_t ld, int32_t box_cols, int32_t box_rows, const char *name);
 // ... of exponent blocks of 512 bytes [row blocks][column blocks], boxes of box_blocks x 2 blocks, no swizzle
 bool scale_map(moe_handle *h, CUtensorMap *map, const void *ptr, int64_t row_blocks, int32_t col_blocks, int32_t box_blocks, const char *name);
 // fused kernel (gemm2_combine.cu)

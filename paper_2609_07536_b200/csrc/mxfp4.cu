@@ -179,7 +179,12 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
 //   warp 1      copies the exponents to TMEM (tcgen05.cp, each of the four lane quarters gets them) and issues
 //               tcgen05.mma.kind::mxf4.block_scale (K = 64, two exponents a row); both are issued by one lane of the converged
 //               warp (pair: of the first CTA) and run in order;
-//   warps 4-11  epilogue: pieces of 32 rows x 32 columns, 16-bit, transposed in registers, 64 contiguous bytes a row.
+//   warps 4-11  epilogue: pieces of 32 rows x 32 columns, 16-bit, transposed in registers, 64 contiguous bytes a row; a pair's, where all
+//               32 rows are the tile's: two warps put 64 columns together in shared memory, which leave as whole lines by a tiled copy
+//               (131072 rows, N 2816, K 2048: 407 -> 386 us at the power limit; half lines straight from registers cost 80 of 407).
+// What bounds a large product: shared memory, which gives the tensor cores 28 KB and takes 31 KB a stage of 400 cycles' MMAs (MMAs alone
+// 185 us, the loads alone 188 us, both 264, with the results 342 us; at the 1000 W limit, where clocks fall to 1.6 GHz, 386 us:
+// 3.9 PFLOP/s), and reads by way of L2 at 15 to 20 TB/s.  With few rows an expert: HBM, 85 to 90 % of the measured copy bandwidth.
 
 constexpr int kPrThreads = 416, kPrEpiWarps = 8;
 constexpr int kPrN = 128;                                   // output columns of a CTA's part of a tile (M of the MMA: a pair's twice that)
@@ -191,6 +196,8 @@ constexpr int kPrScaleCols = 24;                            // TMEM columns of a
 constexpr int kPrTmemCols = 512;
 constexpr int kPrStages = 5;
 constexpr int kMaxExperts = 1024;
+// results on their way out: 32 rows x 64 columns, two of them for every two epilogue warps
+constexpr int kPrOutRows = 32, kPrOutCols = 64, kPrOutBytes = kPrOutRows * kPrOutCols * 2, kPrOutUnits = kPrEpiWarps / 2;
 template <bool kPair>
 struct PrCfg {
     static constexpr int kTileN = kPair ? 2 * kPrN : kPrN;
@@ -198,6 +205,7 @@ struct PrCfg {
     static constexpr int kXBytes = kXRows * kPrK / 2;
     static constexpr int kStageBytes = kPrWBytes + kXBytes + kPrWScaleBytes + kPrXScaleBytes;
     static constexpr int kStages = kPrStages;
+    static constexpr int kOutBytes = kPair ? kPrOutUnits * 2 * kPrOutBytes : 0;
     static constexpr int kRound = kPair ? 32 : 16;                                       // N of the MMA is a multiple of this
     static_assert(kStageBytes % 1024 == 0, "stages are 1024-byte aligned");
 };
@@ -206,6 +214,7 @@ static_assert(2 * kPrRows + kPrStages * kPrScaleCols <= kPrTmemCols, "accumulato
 struct alignas(64) ProductParams {
     CUtensorMap tmW;               // codes [E][N][K / 2]   box 128 bytes x 128 rows, 128B swizzle
     CUtensorMap tmX[3];            // codes [R][K / 2]      box 128 bytes x 192, 64, 16 rows (pair: 96, 32, unused)
+    CUtensorMap tmOut;             // (pair) out [R][N]     box 64 columns x 32 rows, 128B swizzle
     CUtensorMap tmWs, tmXs;        // exponents [row blocks][KQ][512 bytes]   box 1 (x: 2) row blocks x 2 x 512 bytes
     const int32_t *offsets;        // [E + 1]
     void *out;
@@ -470,7 +479,26 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
     __syncwarp();
 }
 
-// The same by one warp, whatever the offsets and however many: a running maximum, clamped to the rows
+// The same piece into shared memory: rows of 128 bytes, 128B swizzle, `half` the columns 32 half .. of the 64
+template <class E>
+__device__ __forceinline__ void stage_piece(const uint32_t (&lo)[16], const uint32_t (&hi)[16], uint32_t buf, int half)
+{
+    const int lane = threadIdx.x & 31, r = lane & 7, chunk = half * 4 + (lane >> 3);
+    const auto pack = [](uint32_t a, uint32_t b) { return RowType<E>::pack(__uint_as_float(a), __uint_as_float(b)); };
+#pragma unroll
+    for (int j = 0; j < 4; ++j)                  // rows 8j..8j+7: four blocks of 8 x 8, stored transposed
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                     ::"r"(buf + (uint32_t)((8 * j + r) * 128 + ((chunk ^ r) << 4))), "r"(pack(lo[4 * j], lo[4 * j + 1])), "r"(pack(lo[4 * j + 2], lo[4 * j + 3])),
+                     "r"(pack(hi[4 * j], hi[4 * j + 1])), "r"(pack(hi[4 * j + 2], hi[4 * j + 3]))
+                     : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"((unsigned long long)map), "r"(src), "r"(x), "r"(y) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+// Row tiles counted by one warp, whatever the offsets and however many: a running maximum, clamped to the rows
 __device__ __noinline__ void repair_offsets(const ProductParams &P, ProductControl *ctl, int lane)
 {
     int tiles = 0, before = 0;
@@ -507,7 +535,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     using C = PrCfg<kPair>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    ProductControl *ctl = reinterpret_cast<ProductControl *>(ring + C::kStages * C::kStageBytes);
+    ProductControl *ctl = reinterpret_cast<ProductControl *>(ring + C::kStages * C::kStageBytes + C::kOutBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = kPair ? cluster_ctarank() : 0u;
     if (threadIdx.x == 0) {
@@ -659,12 +687,20 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     } else if (warp >= 4 && warp < 4 + kPrEpiWarps) {
         const int q4 = warp & 3, grp = (warp - 4) >> 2;
         int it = 0;
+        // a pair: the two warps of 64 columns (a barrier of their own, 1 to 4), and which of their two buffers is next
+        const int unit = 2 * grp + (q4 >> 1);
+        const uint32_t out0 = smem_u32(ring + C::kStages * C::kStageBytes) + (uint32_t)(unit * 2 * kPrOutBytes);
+        uint32_t flip = 0;
         for (; walk.g < total; walk.next(), ++it) {
             const ProductTile t = walk.tile(P, ctl);
             const int a = it & 1, pieces = (t.valid + 31) >> 5, col = t.n0 + (int)rank * kPrN + q4 * 32, cols = P.N - col;
             uint32_t ok = 1u;
             if (lane == 0) ok = pr_wait(smem_u32(&ctl->tmem_full[a]), (uint32_t)(it >> 1) & 1u, ctl, deadline, P.status, (uint32_t)walk.g, 77u) ? 1u : 0u;
-            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            // (the two warps of a unit leave together: each waits for the other in every piece)
+            if (kPair)
+                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %0, 0;\n\tbar.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "+r"(ok) : "r"(1 + unit) : "memory");
+            if (!ok) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(a * kPrRows);
             const auto release = [&]() {
@@ -684,11 +720,26 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
                 tmem_ld_wait(lo);
                 tmem_ld_wait(hi);
                 if (piece + kPrEpiWarps / 4 >= pieces) release();
+                if (kPair && piece * 32 + 32 <= t.valid) {
+                    const int first = col - (q4 & 1) * 32;                     // of the 64 columns
+                    if (first >= P.N) continue;
+                    const bool issues = (q4 & 1) == 0 && lane == 0;
+                    const uint32_t buf = out0 + flip * (uint32_t)kPrOutBytes;
+                    if (issues) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");       // this buffer's last copy has been read
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + unit) : "memory");
+                    stage_piece<E>(lo, hi, buf, q4 & 1);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + unit) : "memory");
+                    if (issues) tma_store_2d(&P.tmOut, buf, first, t.row0 + piece * 32);
+                    flip ^= 1u;
+                    continue;
+                }
                 const int row = piece * 32 + lane;
                 E *dst = row < t.valid && cols > 0 ? static_cast<E *>(P.out) + (long long)(t.row0 + row) * P.ld_out + col : nullptr;
                 store_piece<E>(lo, hi, dst, cols);
             }
         }
+        if (kPair && (q4 & 1) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     // (pair: nobody leaves while the other CTA may still touch its memory)
     tc_fence_before();
@@ -702,7 +753,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
 }
 
 template <bool kPair>
-constexpr size_t pr_smem_bytes() { return (size_t)PrCfg<kPair>::kStages * PrCfg<kPair>::kStageBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127); }
+constexpr size_t pr_smem_bytes() { return (size_t)PrCfg<kPair>::kStages * PrCfg<kPair>::kStageBytes + PrCfg<kPair>::kOutBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127); }
 static_assert(pr_smem_bytes<false>() <= 227 * 1024 && pr_smem_bytes<true>() <= 227 * 1024, "the product's stages exceed the shared memory of an SM");
 
 // Mean rows per expert from which tiles by pairs of CTAs pay: they read less per product, but there are half as many places for them.
@@ -847,6 +898,7 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     const int32_t boxes[3] = {pair ? PrCfg<true>::kXRows : PrCfg<false>::kXRows, pair ? 32 : 64, 16};
     for (int i = 0; i < (pair ? 2 : 3); ++i)
         if (!code_map(h, &p.tmX[i], x_codes, 0, rows, K / 2, boxes[i], "x_codes")) return MOE_ERR_CUDA;
+    if (pair && !out_map(h, &p.tmOut, out, rows, N, ld_out, kPrOutCols, kPrOutRows, "out")) return MOE_ERR_CUDA;
     if (!code_map(h, &p.tmW, w_codes, E_tot, N, K / 2, kPrN, "w_codes") ||
         !scale_map(h, &p.tmXs, x_scales, scale_blocks(rows, E_tot), p.KQ, 2, "x_scales") ||
         !scale_map(h, &p.tmWs, w_scales, scale_blocks((int64_t)E_tot * N, E_tot), p.KQ, 1, "w_scales"))
