@@ -559,49 +559,55 @@ def moe_mxfp4_scale_bytes(rows: int, K: int, groups: int) -> int:
     return b.value
 
 
-def _mxfp4_operand(codes, scales, groups, dev, who, what=""):
-    """(address of the codes, address of the exponents, rows, K); codes uint8 [..., K / 2] contiguous."""
-    half, n = codes.shape[-1], codes.numel()
-    rows, K = n // max(1, half), 2 * half
-    need = (rows // 128 + groups) * ((K + 127) // 128) * 512            # moe_mxfp4_scale_bytes, whose checks the call repeats
-    return (_vector(codes, n, _u8, dev, who, what + "codes"), _vector(scales, need, _u8, dev, who, what + "scales"), rows, K)
+def _mxfp4_bytes(rows, K, groups):
+    """moe_mxfp4_scale_bytes, whose checks the calls repeat."""
+    return (rows // 128 + groups) * ((K + 127) // 128) * 512
 
 
 def moe_mxfp4_quantize(h, src, codes, scales, groups, status_dev, offsets=None, inv_perm=None, stream=None):
     """src [rows, K] -> codes uint8 [rows, K / 2] and scales (moe_mxfp4_scale_bytes) in `groups` groups: by offsets int32
     [groups + 1], or of equally many rows.  inv_perm int32 [T, copies]: src is [T, K], row t goes to the rows inv_perm[t]."""
     who, dev = "moe_mxfp4_quantize", _device()
-    c, sc, rows, K = _mxfp4_operand(codes, scales, groups, dev, who)
-    copies = 1 if inv_perm is None else inv_perm.shape[-1]
-    if inv_perm is not None and inv_perm.numel() != rows:
-        raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm names {inv_perm.numel()} rows, codes have {rows}")
-    a, lda = _matrix(src, rows // max(1, copies), K, src.dtype, dev, who, "src")
-    _check((_lib or lib()).moe_mxfp4_quantize(h, a, lda, _row_type(src.dtype, who), rows, K, groups, _vector(offsets, groups + 1, _i32, dev, who, "offsets"),
-                                    _vector(inv_perm, rows, _i32, dev, who, "inv_perm"), copies, c, sc, _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
+    half, n = codes.shape[-1], codes.numel()
+    rows, K, copies = n // max(1, half), 2 * half, 1
+    if inv_perm is not None:
+        copies = inv_perm.shape[-1]
+        if inv_perm.numel() != rows or copies < 1:
+            raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm names {inv_perm.numel()} rows, codes have {rows}")
+    kind = src.dtype
+    a, lda = _matrix(src, rows // copies, K, kind, dev, who, "src")
+    _check((_lib or lib()).moe_mxfp4_quantize(
+        h, a, lda, _row_type(kind, who), rows, K, groups, _vector(offsets, groups + 1, _i32, dev, who, "offsets"), _vector(inv_perm, rows, _i32, dev, who, "inv_perm"),
+        copies, _vector(codes, n, _u8, dev, who, "codes"), _vector(scales, _mxfp4_bytes(rows, K, groups), _u8, dev, who, "scales"),
+        _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
 
 
 def moe_mxfp4_dequantize(h, codes, scales, groups, out, status_dev, offsets=None, stream=None):
     """out [rows, K] = the values that codes and scales stand for."""
     who, dev = "moe_mxfp4_dequantize", _device()
-    c, sc, rows, K = _mxfp4_operand(codes, scales, groups, dev, who)
-    a, lda = _matrix(out, rows, K, out.dtype, dev, who, "out")
-    _check((_lib or lib()).moe_mxfp4_dequantize(h, c, sc, rows, K, groups, _vector(offsets, groups + 1, _i32, dev, who, "offsets"), _row_type(out.dtype, who),
-                                      a, lda, _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
+    half, n, kind = codes.shape[-1], codes.numel(), out.dtype
+    rows, K = n // max(1, half), 2 * half
+    a, lda = _matrix(out, rows, K, kind, dev, who, "out")
+    _check((_lib or lib()).moe_mxfp4_dequantize(
+        h, _vector(codes, n, _u8, dev, who, "codes"), _vector(scales, _mxfp4_bytes(rows, K, groups), _u8, dev, who, "scales"), rows, K, groups,
+        _vector(offsets, groups + 1, _i32, dev, who, "offsets"), _row_type(kind, who), a, lda, _vector(status_dev, 4, _i32, dev, who, "status_dev"),
+        _raw_stream(stream, dev)), who, h)
 
 
 def moe_mxfp4_gemm(h, x_codes, x_scales, w_codes, w_scales, offsets, out, status_dev, stream=None):
     """out[r] = w[e] x[r] for the rows r of expert e, offsets[e] <= r < offsets[e + 1]; w_codes uint8 [E_tot, N, K / 2]."""
     who, dev = "moe_mxfp4_gemm", _device()
-    if len(w_codes.shape) != 3 or len(x_codes.shape) != 2:
-        raise MoeError(MOE_ERR_SHAPE, who, "w_codes is [E_tot, N, K / 2], x_codes [rows, K / 2]")
-    E, N = w_codes.shape[0], w_codes.shape[1]
-    w, ws, w_rows, Kw = _mxfp4_operand(w_codes, w_scales, E, dev, who, "w_")
-    x, xs, rows, K = _mxfp4_operand(x_codes, x_scales, E, dev, who, "x_")
-    if K != Kw:
-        raise MoeError(MOE_ERR_SHAPE, who, f"x has {K} columns, w {Kw}")
-    a, lda = _matrix(out, rows, N, out.dtype, dev, who, "out")
-    _check((_lib or lib()).moe_mxfp4_gemm(h, x, xs, w, ws, _vector(offsets, E + 1, _i32, dev, who, "offsets"), rows, E, N, K, _row_type(out.dtype, who), a, lda,
-                                _vector(status_dev, 4, _i32, dev, who, "status_dev"), _raw_stream(stream, dev)), who, h)
+    w_shape, x_shape, kind = w_codes.shape, x_codes.shape, out.dtype
+    if len(w_shape) != 3 or len(x_shape) != 2 or w_shape[2] != x_shape[1]:
+        raise MoeError(MOE_ERR_SHAPE, who, f"w_codes is {tuple(w_shape)}, x_codes {tuple(x_shape)}, not [E_tot, N, K / 2] and [rows, K / 2]")
+    E, N, half = w_shape
+    rows, K = x_shape[0], 2 * half
+    a, lda = _matrix(out, rows, N, kind, dev, who, "out")
+    _check((_lib or lib()).moe_mxfp4_gemm(
+        h, _vector(x_codes, 0, _u8, dev, who, "x_codes"), _vector(x_scales, _mxfp4_bytes(rows, K, E), _u8, dev, who, "x_scales"),
+        _vector(w_codes, 0, _u8, dev, who, "w_codes"), _vector(w_scales, _mxfp4_bytes(E * N, K, E), _u8, dev, who, "w_scales"),
+        _vector(offsets, E + 1, _i32, dev, who, "offsets"), rows, E, N, K, _row_type(kind, who), a, lda, _vector(status_dev, 4, _i32, dev, who, "status_dev"),
+        _raw_stream(stream, dev)), who, h)
 
 
 # ----------------------------------------------------------------------------- device memory plumbing

@@ -182,9 +182,10 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
 //   warps 4-11  epilogue: pieces of 32 rows x 32 columns, 16-bit, transposed in registers, 64 contiguous bytes a row; a pair's, where all
 //               32 rows are the tile's: two warps put 64 columns together in shared memory, which leave as whole lines by a tiled copy
 //               (131072 rows, N 2816, K 2048: 407 -> 386 us at the power limit; half lines straight from registers cost 80 of 407).
-// What bounds a large product: shared memory, which gives the tensor cores 28 KB and takes 31 KB a stage of 400 cycles' MMAs (MMAs alone
-// 185 us, the loads alone 188 us, both 264, with the results 342 us; at the 1000 W limit, where clocks fall to 1.6 GHz, 386 us:
-// 3.9 PFLOP/s), and reads by way of L2 at 15 to 20 TB/s.  With few rows an expert: HBM, 85 to 90 % of the measured copy bandwidth.
+// What bounds a large product: shared memory.  In a stage of a pair the MMAs read 40 KB (4 KB of weights and 6 KB of rows each), the copies
+// write 31, results pass through with 12: 83 KB at 128 bytes a cycle are 650 cycles, where the MMAs alone take 400.  131072 rows, N 2816,
+// K 2048: MMAs alone 185 us, copies of the weights and of the rows +45 each, results +65: 342 us, 4.4 PFLOP/s; 386 us at the 1000 W limit,
+// where clocks fall to 1.6 GHz.  With few rows an expert it is HBM: 85 to 90 % of the measured copy bandwidth.
 
 constexpr int kPrThreads = 416, kPrEpiWarps = 8;
 constexpr int kPrN = 128;                                   // output columns of a CTA's part of a tile (M of the MMA: a pair's twice that)
