@@ -564,16 +564,18 @@ def _mxfp4_bytes(rows, K, groups):
     return (rows // 128 + groups) * ((K + 127) // 128) * 512
 
 
-def moe_mxfp4_quantize(h, src, codes, scales, groups, status_dev, offsets=None, inv_perm=None, stream=None):
+def moe_mxfp4_quantize(h, src, codes, scales, groups, status_dev, offsets=None, inv_perm=None, copies=None, stream=None):
     """src [rows, K] -> codes uint8 [rows, K / 2] and scales (moe_mxfp4_scale_bytes) in `groups` groups: by offsets int32
-    [groups + 1], or of equally many rows.  inv_perm int32 [T, copies]: src is [T, K], row t goes to the rows inv_perm[t]."""
+    [groups + 1], or of equally many rows.  inv_perm int32 [T, copies], or its address with `copies`: src is [T, K], row t goes to the
+    rows inv_perm[t]."""
     who, dev = "moe_mxfp4_quantize", _device()
     half, n = codes.shape[-1], codes.numel()
-    rows, K, copies = n // max(1, half), 2 * half, 1
-    if inv_perm is not None:
-        copies = inv_perm.shape[-1]
-        if inv_perm.numel() != rows or copies < 1:
+    rows, K = n // max(1, half), 2 * half
+    if inv_perm is not None and not isinstance(inv_perm, int):
+        if inv_perm.numel() != rows or copies not in (None, inv_perm.shape[-1]):
             raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm names {inv_perm.numel()} rows, codes have {rows}")
+        copies = inv_perm.shape[-1]
+    copies = max(1, copies or 1)
     kind = src.dtype
     a, lda = _matrix(src, rows // copies, K, kind, dev, who, "src")
     _check((_lib or lib()).moe_mxfp4_quantize(

@@ -468,7 +468,7 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
             ready = mbar_test_wait(empty_bar, phase ^ 1u);
         }
     }
-    if (!ok && rank == 0) {
+    if ((!ok || ctl->abort) && rank == 0) {
         // wind-down: the copies already issued land before shared memory is released
         const int stage = (int)(empty_bar - empty0) >> 3;
         const unsigned long long drain = globaltimer_ns() + 2000000ull;

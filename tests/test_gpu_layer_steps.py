@@ -527,6 +527,23 @@ def test_product_past_32_bits():
     assert st.tolist() == [0, 0, 0, 0]
 
 
+def test_product_of_many_experts_past_32_bits():
+    R, N, K, E = 255000, 8456, 32, 1000                 # 2.16e9 elements out, 255 rows an expert
+    offsets = ints([255 * e for e in range(E + 1)])
+    codes = torch.randint(0, 256, (R, K // 2), dtype=torch.uint8, device="cuda")
+    xs = torch.full((B.moe_mxfp4_scale_bytes(R, K, E),), 127, dtype=torch.uint8, device="cuda")
+    wc = torch.randint(0, 256, (E, N, K // 2), dtype=torch.uint8, device="cuda")
+    ws = torch.full((B.moe_mxfp4_scale_bytes(E * N, K, E),), 127, dtype=torch.uint8, device="cuda")
+    out, st = torch.empty((R, N), dtype=torch.bfloat16, device="cuda"), status()
+    B.moe_mxfp4_gemm(handle(), codes, xs, wc, ws, offsets, out, st)
+    for e in (0, 500, 999):
+        at = 255 * e + 250
+        x = ref.dequantize(codes[at:at + 5].cpu().numpy(), np.full((5, 1), 127, np.uint8))
+        want = x @ ref.dequantize(wc[e].cpu().numpy(), np.full((N, 1), 127, np.uint8)).T     # multiples of 1/4 below 2^11: exact in fp32
+        assert (np.abs(f64(out[at:at + 5]) - want) <= half_step(torch.bfloat16, want)).all()
+    assert st.tolist() == [0, 0, 0, 0]
+
+
 # ----------------------------------------------------------------------------- together
 
 def routed(T, k, E, seed):
@@ -767,3 +784,64 @@ def test_tensors_that_do_not_fit_together_are_refused():
     refused(B.MOE_ERR_UNSUPPORTED, B.moe_mxfp4_gemm, half, mx, wc, wsc, ints([0, 4, 8]), torch.zeros((8, 16), device="cuda"), st)
     refused(B.MOE_ERR_SHAPE, B.moe_mxfp4_gemm, half, mx, wc, wsc, ints([0, 8]), torch.zeros((8, 16), **bf), st)
     B.moe_mxfp4_gemm(h, half, mx, wc, wsc, ints([0, 4, 8]), torch.zeros((8, 16), **bf), st)
+
+
+def test_addresses_in_place_of_index_tensors():
+    # the routing arrays as the library's own view names them: by address
+    T, k, E, H = 40, 3, 7, 96
+    h, s, st = handle(), shape_of(T, k, H), status()
+    ws_keep, inv, offsets, _ = routed(T, k, E, 3)
+    tokens = normal((T, H), torch.bfloat16, 1).cuda()
+    rows = [torch.zeros((T * k, H), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    B.moe_permute(h, tokens, inv, s, rows[0], st)
+    B.moe_permute(h, tokens, inv.data_ptr(), s, rows[1], st)
+    assert torch.equal(*rows)
+    codes = [torch.zeros((T * k, H // 2), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros(B.moe_mxfp4_scale_bytes(T * k, H, E), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    B.moe_mxfp4_quantize(h, tokens, codes[0], scales[0], E, st, offsets=offsets, inv_perm=inv)
+    B.moe_mxfp4_quantize(h, tokens, codes[1], scales[1], E, st, offsets=offsets.data_ptr(), inv_perm=inv.data_ptr(), copies=k)
+    assert torch.equal(*codes) and torch.equal(*scales) and st.tolist() == [0, 0, 0, 0]
+
+
+def test_nothing_to_do():
+    h, st = handle(), status()
+    none = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, dtype=dtype, device="cuda")  # noqa: E731
+    s = shape_of(0, 4, 64)
+    B.moe_permute(h, none(0, 64), none(0, 4, dtype=torch.int32), s, none(0, 64), st)
+    B.moe_unpermute_grad(h, none(0, 64), none(0, 64), none(0, 4, dtype=torch.int32), none(0, 4, dtype=torch.float32), s, none(0, 64), none(0, 4, dtype=torch.float32), st)
+    B.moe_gated_act(h, none(0, 64), none(0, 32), none(0, 64, dtype=torch.uint8), none(0, 2, dtype=torch.uint8))
+    scales = none(B.moe_mxfp4_scale_bytes(0, 64, 2), dtype=torch.uint8)
+    B.moe_mxfp4_quantize(h, none(0, 64), none(0, 32, dtype=torch.uint8), scales, 2, st, offsets=ints([0, 0, 0]))
+    w, ws = none(2, 16, 32, dtype=torch.uint8), none(B.moe_mxfp4_scale_bytes(32, 64, 2), dtype=torch.uint8)
+    B.moe_mxfp4_gemm(h, none(0, 32, dtype=torch.uint8), scales, w, ws, ints([0, 0, 0]), none(0, 16), st)
+    # rows that there are, but none of them in a group
+    out = torch.full((5, 16), 7.0, dtype=torch.bfloat16, device="cuda")
+    x, xs = torch.zeros((5, 32), dtype=torch.uint8, device="cuda"), torch.zeros(B.moe_mxfp4_scale_bytes(5, 64, 2), dtype=torch.uint8, device="cuda")
+    B.moe_mxfp4_gemm(h, x, xs, w, ws, ints([0, 0, 0]), out, st)
+    assert (out == 7.0).all() and st.tolist() == [0, 0, 0, 0]
+
+
+def test_a_status_buffer_on_the_host_is_refused():
+    h, s = handle(), shape_of(4, 2, 64)
+    tokens, rows, inv = torch.zeros((4, 64), device="cuda"), torch.zeros((8, 64), device="cuda"), torch.zeros((4, 2), dtype=torch.int32, device="cuda")
+    with pytest.raises(B.MoeError) as e:
+        B.moe_permute(h, tokens, inv, s, rows, torch.zeros(4, dtype=torch.int32))
+    assert e.value.code == B.MOE_ERR_UNSUPPORTED
+
+
+def test_products_on_two_streams_at_once():
+    # both families of tiles beside each other and beside the row kernels, against the same calls one after the other
+    small, large = [0, 5, 9, 30], [0, 400, 401, 900]
+    jobs = []
+    for offsets, N, K, seed in ((small, 264, 320, 1), (large, 264, 320, 2)):
+        xc, xs, wc, ws, _, _ = product_case(offsets, offsets[-1], N, K, seed)
+        jobs.append((xc, xs, wc, ws, ints(offsets), [torch.zeros((offsets[-1], N), dtype=torch.bfloat16, device="cuda") for _ in range(2)], status(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for which in range(2):
+        for _ in range(20 if which else 1):
+            for xc, xs, wc, ws, off, out, st, stream in jobs:
+                with torch.cuda.stream(stream if which else torch.cuda.current_stream()):
+                    B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, off, out[which], st)
+        torch.cuda.synchronize()
+    for *_, out, st, stream in jobs:
+        assert torch.equal(*out) and st.tolist() == [0, 0, 0, 0]
