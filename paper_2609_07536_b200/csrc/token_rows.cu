@@ -16,7 +16,8 @@
 namespace moe {
 namespace {
 
-constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
+constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32;
+constexpr int kGradThreads = 64, kGradWarps = kGradThreads / 32;       // the way back's gradient
 
 struct TokenRows {
     const int32_t *inv_perm;
@@ -65,7 +66,7 @@ __global__ void __launch_bounds__(kRowThreads) spread_kernel(const __grid_consta
 // way, so that the one latency does not lie in front of the other in every piece (16384 tokens, 8 rows each of 4 KB: 95 us, 98 % of the
 // measured copy bandwidth; a block for every eight pieces 107).
 template <class E, bool kWeighted, int kAhead>
-__global__ void __launch_bounds__(kRowThreads, kAhead == 8 ? 3 : 4) gather_kernel(const __grid_constant__ TokenRows p, const E *rows, E *tokens)
+__global__ void __launch_bounds__(kRowThreads, kAhead == 8 ? 6 : 8) gather_kernel(const __grid_constant__ TokenRows p, const E *rows, E *tokens)
 {
     grid_dependency_wait();
     constexpr int kVec = RowType<E>::kVec;
@@ -120,15 +121,15 @@ __global__ void __launch_bounds__(kRowThreads, kAhead == 8 ? 3 : 4) gather_kerne
     }
 }
 
-// A warp per assignment, four vectors of both inputs in flight a thread: the warps of a block share the token's d_out through L1 (16384
-// tokens, 8 rows each of 4 KB: 178 us, 98 % of the measured copy bandwidth; one vector at a time 206).
+// A warp per assignment, four vectors of both inputs in flight a thread: blocks of two warps start as soon as two others
+// are done (16384 tokens, 8 rows each of 4 KB: 174 us at the measured copy bandwidth; eight warps a block 178, one vector at a time 206).
 template <class E>
-__global__ void __launch_bounds__(kRowThreads) spread_grad_kernel(const __grid_constant__ TokenRows p, const E *d_out, const E *rows, E *d_rows, float *d_w)
+__global__ void __launch_bounds__(kGradThreads) spread_grad_kernel(const __grid_constant__ TokenRows p, const E *d_out, const E *rows, E *d_rows, float *d_w)
 {
     grid_dependency_wait();
     constexpr int kVec = RowType<E>::kVec, kAhead = 4;
     const int lane = threadIdx.x & 31;
-    for (long long f = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5); f < p.pieces; f += (long long)gridDim.x * kRowWarps) {
+    for (long long f = (long long)blockIdx.x * kGradWarps + (threadIdx.x >> 5); f < p.pieces; f += (long long)gridDim.x * kGradWarps) {
         const long long t = f / p.k_tot;
         const int r = __shfl_sync(0xffffffffu, lane == 0 ? row_of(p, f) : 0, 0);
         float dot = 0.0f;
@@ -191,9 +192,9 @@ int32_t token_rows_args(moe_handle *h, const moe_shape *s, int32_t dtype, const 
     if (p->pieces >= (int64_t)1 << 32) return MOE_ERR_SHAPE;
     return MOE_OK;
 }
-unsigned row_grid(const TokenRows &p)
+unsigned row_grid(const TokenRows &p, int warps = kRowWarps)
 {
-    const long long blocks = (p.pieces + kRowWarps - 1) / kRowWarps;
+    const long long blocks = (p.pieces + warps - 1) / warps;
     return (unsigned)(blocks < (1ll << 30) ? blocks : 1ll << 30);
 }
 
@@ -239,7 +240,7 @@ extern "C" int32_t moe_permute_grad(moe_handle *h, const void *d_rows, int64_t l
     if ((rc = require_handle_device(h, "moe_permute_grad")) != MOE_OK) return rc;
     return with_row_type(dtype, [&](auto *e) -> int32_t {
         using E = std::remove_pointer_t<decltype(e)>;
-        const cudaError_t err = launch_chained(p.k_tot > 4 ? gather_kernel<E, false, 8> : gather_kernel<E, false, 4>, staying_grid(h, p, p.k_tot > 4 ? 3 : 4), kRowThreads, 0, static_cast<cudaStream_t>(stream), p, typed<E>(d_rows), typed<E>(d_tokens));
+        const cudaError_t err = launch_chained(p.k_tot > 4 ? gather_kernel<E, false, 8> : gather_kernel<E, false, 4>, staying_grid(h, p, p.k_tot > 4 ? 6 : 8), kRowThreads, 0, static_cast<cudaStream_t>(stream), p, typed<E>(d_rows), typed<E>(d_tokens));
         return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "permute gradient launch");
     });
 }
@@ -256,7 +257,7 @@ extern "C" int32_t moe_unpermute(moe_handle *h, const void *rows, int64_t ld_row
     if ((rc = require_handle_device(h, "moe_unpermute")) != MOE_OK) return rc;
     return with_row_type(dtype, [&](auto *e) -> int32_t {
         using E = std::remove_pointer_t<decltype(e)>;
-        const cudaError_t err = launch_chained(p.k_tot > 4 ? gather_kernel<E, true, 8> : gather_kernel<E, true, 4>, staying_grid(h, p, p.k_tot > 4 ? 3 : 4), kRowThreads, 0, static_cast<cudaStream_t>(stream), p, typed<E>(rows), typed<E>(out));
+        const cudaError_t err = launch_chained(p.k_tot > 4 ? gather_kernel<E, true, 8> : gather_kernel<E, true, 4>, staying_grid(h, p, p.k_tot > 4 ? 6 : 8), kRowThreads, 0, static_cast<cudaStream_t>(stream), p, typed<E>(rows), typed<E>(out));
         return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "unpermute launch");
     });
 }
@@ -278,7 +279,7 @@ extern "C" int32_t moe_unpermute_grad(moe_handle *h, const void *d_out, int64_t 
     if ((rc = require_handle_device(h, "moe_unpermute_grad")) != MOE_OK) return rc;
     return with_row_type(dtype, [&](auto *e) -> int32_t {
         using E = std::remove_pointer_t<decltype(e)>;
-        const cudaError_t err = launch_chained(spread_grad_kernel<E>, row_grid(p), kRowThreads, 0, static_cast<cudaStream_t>(stream), p, typed<E>(d_out), typed<E>(rows), typed<E>(d_rows), d_topk_w);
+        const cudaError_t err = launch_chained(spread_grad_kernel<E>, row_grid(p, kGradWarps), kGradThreads, 0, static_cast<cudaStream_t>(stream), p, typed<E>(d_out), typed<E>(rows), typed<E>(d_rows), d_topk_w);
         return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "unpermute gradient launch");
     });
 }
