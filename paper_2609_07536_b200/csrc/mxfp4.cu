@@ -196,7 +196,8 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
 // out[r][n] = sum_k x[r][k] w[e][n][k] for the rows r of expert e, fp32 accumulation in TMEM, one rounding at the end.
 // The weights are on the M side of the MMA and the rows on its N side, as in the other products here: a tile costs what its rows cost.
 // Tile: 128 columns of the output x up to 192 rows, or, computed by a pair of CTAs (cta_group::2), 256 columns x up to 192 rows: each CTA
-// then loads its own 128 rows of the weights and half of the rows of x, 31 KB a stage instead of 43 for the same products.
+// then loads its own 128 rows of the weights and half of the rows of x, 31 KB a stage instead of 43 for the same products.  Where experts
+// have few rows: 128 columns x up to 64 rows, in eight stages instead of five.
 // TMEM holds two accumulators of 192 columns and, for five stages, 24 columns of exponents (128 rows of weights: 4 per 128
 // columns of K; 256 rows of x: 8; a pair's CTAs each have those of all rows of x); that is 504 of its 512 columns, and why a tile has
 // 192 rows and not 256.  A stage is 256 columns of K: 128 bytes of codes a row, a swizzle row.
@@ -214,34 +215,39 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
 
 constexpr int kPrThreads = 416, kPrEpiWarps = 8;
 constexpr int kPrN = 128;                                   // output columns of a CTA's part of a tile (M of the MMA: a pair's twice that)
-constexpr int kPrRows = 192;                                // rows of a tile (N of the MMA)
 constexpr int kPrK = 256, kPrStepK = 64;                    // columns of K of a stage, of an MMA
 constexpr int kPrWBytes = kPrN * kPrK / 2;
 constexpr int kPrWScaleBytes = 2 * kMxTileBytes, kPrXScaleBytes = 4 * kMxTileBytes;      // x: row block 0 of both 128s of K, then row block 1
 constexpr int kPrScaleCols = 24;                            // TMEM columns of a stage's exponents: weights 2 x 4, rows 2 x 8
 constexpr int kPrTmemCols = 512;
-constexpr int kPrStages = 5;
+constexpr int kPrMaxStages = 8;
 constexpr int kMaxExperts = 1024;
 // results on their way out: 32 rows x 64 columns, two of them for every two epilogue warps
 constexpr int kPrOutRows = 32, kPrOutCols = 64, kPrOutBytes = kPrOutRows * kPrOutCols * 2, kPrOutUnits = kPrEpiWarps / 2;
-template <bool kPair>
+// Families of tiles: one CTA; a pair; one CTA where an expert has few rows: 64 rows of x at most leave shared memory and TMEM for eight
+// stages, and it is bytes in flight that a product of few rows lives on
+enum { kOneTiles, kPairTiles, kFewTiles };
+template <int kKind>
 struct PrCfg {
+    static constexpr bool kPair = kKind == kPairTiles, kFew = kKind == kFewTiles;
     static constexpr int kTileN = kPair ? 2 * kPrN : kPrN;
-    static constexpr int kXRows = kPair ? kPrRows / 2 : kPrRows;                         // rows of x that a CTA holds
+    static constexpr int kRows = kFew ? 64 : 192;                                        // rows of a tile (N of the MMA)
+    static constexpr int kXRows = kPair ? kRows / 2 : kRows;                             // rows of x that a CTA holds
     static constexpr int kXBytes = kXRows * kPrK / 2;
+    static constexpr int kXsBytes = kFew ? kPrXScaleBytes / 2 : kPrXScaleBytes;          // what comes of the exponents: 64 rows lie in one row block
     static constexpr int kStageBytes = kPrWBytes + kXBytes + kPrWScaleBytes + kPrXScaleBytes;
-    static constexpr int kStages = kPrStages;
+    static constexpr int kStages = kFew ? kPrMaxStages : 5;
     static constexpr int kOutBytes = kPair ? kPrOutUnits * 2 * kPrOutBytes : 0;
     static constexpr int kRound = kPair ? 32 : 16;                                       // N of the MMA is a multiple of this
     static_assert(kStageBytes % 1024 == 0, "stages are 1024-byte aligned");
+    static_assert(2 * kRows + kStages * kPrScaleCols <= kPrTmemCols, "accumulators and exponents exceed TMEM");
 };
-static_assert(2 * kPrRows + kPrStages * kPrScaleCols <= kPrTmemCols, "accumulators and exponents exceed TMEM");
 
 struct alignas(64) ProductParams {
     CUtensorMap tmW;               // codes [E][N][K / 2]   box 128 bytes x 128 rows, 128B swizzle
-    CUtensorMap tmX[3];            // codes [R][K / 2]      box 128 bytes x 192, 64, 16 rows (pair: 96, 32, unused)
+    CUtensorMap tmX[3];            // codes [R][K / 2]      box 128 bytes x 192, 64, 16 rows (pair: 96, 32; few rows: 64, 16)
     CUtensorMap tmOut;             // (pair) out [R][N]     box 64 columns x 32 rows, 128B swizzle
-    CUtensorMap tmWs, tmXs;        // exponents [row blocks][KQ][512 bytes]   box 1 (x: 2) row blocks x 2 x 512 bytes
+    CUtensorMap tmWs, tmXs;        // exponents [row blocks][KQ][512 bytes]   box 1 (x: 2; few rows: 1) row blocks x 2 x 512 bytes
     const int32_t *offsets;        // [E + 1]
     void *out;
     long long ld_out;              // elements
@@ -251,7 +257,7 @@ struct alignas(64) ProductParams {
     Divisor by_NT;
 };
 struct ProductControl {
-    unsigned long long full[kPrStages], empty[kPrStages], tmem_full[2], tmem_empty[2], drain;
+    unsigned long long full[kPrMaxStages], empty[kPrMaxStages], tmem_full[2], tmem_empty[2], drain;
     uint32_t tmem_base;
     volatile uint32_t abort;
     int32_t warp_tiles[kPrThreads / 32];
@@ -283,8 +289,9 @@ __device__ __forceinline__ bool pr_wait(uint32_t bar, uint32_t parity, ProductCo
 struct ProductTile {
     int e, row0, valid, local, n0;     // local: first row inside the expert
 };
-template <bool kPair>
+template <int kKind>
 struct ProductWalk {
+    static constexpr bool kPair = kKind == kPairTiles;
     int g, e;
     // (the whole warp)
     __device__ __forceinline__ ProductWalk(const ProductParams &P, const ProductControl *ctl) : g((int)blockIdx.x >> (kPair ? 1 : 0)), e(-1)
@@ -299,10 +306,10 @@ struct ProductWalk {
         while (ctl->tiles[e + 1] <= mu) ++e;       // (g is a tile that there is)
         ProductTile t;
         t.e = e;
-        t.local = (mu - ctl->tiles[e]) * kPrRows;
+        t.local = (mu - ctl->tiles[e]) * PrCfg<kKind>::kRows;
         t.row0 = ctl->first[e] + t.local;
-        t.valid = min(kPrRows, ctl->first[e + 1] - t.row0);
-        t.n0 = (g - mu * P.NT) * PrCfg<kPair>::kTileN;
+        t.valid = min(PrCfg<kKind>::kRows, ctl->first[e + 1] - t.row0);
+        t.n0 = (g - mu * P.NT) * PrCfg<kKind>::kTileN;
         return t;
     }
 };
@@ -419,11 +426,12 @@ __device__ __forceinline__ void store_piece(const uint32_t (&lo)[16], const uint
 // take 400; an untiled copy takes longer than a tiled one.)  Pair: every copy completes on the first CTA's barrier, at the same
 // offset there, and that CTA's loaders arm it for both.
 enum { kLoadW, kLoadX, kLoadWs, kLoadXs };
-template <bool kPair, int kWhat>
-__device__ __forceinline__ void product_loader(const ProductParams &P, ProductControl *ctl, ProductWalk<kPair> walk, int total, unsigned long long deadline,
+template <int kKind, int kWhat>
+__device__ __forceinline__ void product_loader(const ProductParams &P, ProductControl *ctl, ProductWalk<kKind> walk, int total, unsigned long long deadline,
                                                uint32_t rank, uint8_t *ring)
 {
-    using C = PrCfg<kPair>;
+    using C = PrCfg<kKind>;
+    constexpr bool kPair = C::kPair;
     constexpr uint32_t kAt = kWhat == kLoadW ? 0 : kWhat == kLoadX ? kPrWBytes : kWhat == kLoadWs ? kPrWBytes + C::kXBytes : kPrWBytes + C::kXBytes + kPrWScaleBytes;
     constexpr int kStep = kWhat == kLoadW || kWhat == kLoadX ? kPrK / 2 : 2;
     const uint32_t dst0 = smem_u32(ring) + kAt, empty0 = smem_u32(&ctl->empty[0]), full0 = smem_u32(&ctl->full[0]);
@@ -442,10 +450,10 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
         } else if (kWhat == kLoadX) {
             // rows that this CTA holds of the tile: in one box, or in two of 64; those behind the tile's own are read for nothing
             const int held = kPair ? ((t.valid + C::kRound - 1) & -C::kRound) / 2 : t.valid;
-            const int which = kPair ? (held > 32 ? 0 : 1) : held > 128 ? 0 : held > 16 ? 1 : 2;
-            boxes = !kPair && which == 1 && held > 64 ? 2 : 1;
+            const int which = kPair ? (held > 32 ? 0 : 1) : C::kFew ? (held > 16 ? 0 : 1) : held > 128 ? 0 : held > 16 ? 1 : 2;
+            boxes = kKind == kOneTiles && which == 1 && held > 64 ? 2 : 1;
             map = &P.tmX[which];
-            bytes = (which == 0 ? C::kXRows : which == 1 ? (kPair ? 32u : 64u) : 16u) * (kPrK / 2);
+            bytes = (which == 0 ? C::kXRows : which == 2 || C::kFew ? 16u : kPair ? 32u : 64u) * (kPrK / 2);
             y = t.row0 + (int)rank * held;
         } else if (kWhat == kLoadWs) {
             map = &P.tmWs;
@@ -454,7 +462,7 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
         } else {
             // the row block that the quantisation put the tile's first row into: by the expert's first row (row0 - local)
             map = &P.tmXs;
-            bytes = kPrXScaleBytes;
+            bytes = C::kXsBytes;
             y = (t.row0 - t.local) / kMxTile + t.e + t.local / kMxTile;
         }
         const uint32_t expected = (kPair ? 2u : 1u) * (uint32_t)boxes * bytes;
@@ -470,7 +478,7 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
                 if (kWhat == kLoadX) {
                     if (kPair) tma_load_2d_pair(dst, map, bar, x, y);
                     else tma_load_2d(dst, map, bar, x, y);
-                    if (!kPair && boxes == 2) tma_load_2d(dst + bytes, map, bar, x, y + 64);
+                    if (kKind == kOneTiles && boxes == 2) tma_load_2d(dst + bytes, map, bar, x, y + 64);
                 } else if (kWhat == kLoadW) {
                     if (kPair) tma_load_3d_pair(dst, map, bar, x, y, z);
                     else tma_load_3d(dst, map, bar, x, y, z);
@@ -525,7 +533,7 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
 }
 
 // Row tiles counted by one warp, whatever the offsets and however many: a running maximum, clamped to the rows
-__device__ __noinline__ void repair_offsets(const ProductParams &P, ProductControl *ctl, int lane)
+__device__ __noinline__ void repair_offsets(const ProductParams &P, ProductControl *ctl, int lane, int tile_rows)
 {
     int tiles = 0, before = 0;
     for (int e0 = 0; e0 <= P.E; e0 += 32) {
@@ -540,7 +548,7 @@ __device__ __noinline__ void repair_offsets(const ProductParams &P, ProductContr
         int prev = __shfl_up_sync(0xffffffffu, o, 1);
         if (lane == 0) prev = before;
         // row tiles of the expert that ends at `o` (expert e - 1)
-        int t = (e > 0 && e <= P.E) ? (o - prev + kPrRows - 1) / kPrRows : 0;
+        int t = (e > 0 && e <= P.E) ? (o - prev + tile_rows - 1) / tile_rows : 0;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int u = __shfl_up_sync(0xffffffffu, t, d);
@@ -555,10 +563,11 @@ __device__ __noinline__ void repair_offsets(const ProductParams &P, ProductContr
     }
 }
 
-template <class E, bool kPair>
+template <class E, int kKind>
 __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __grid_constant__ ProductParams P)
 {
-    using C = PrCfg<kPair>;
+    using C = PrCfg<kKind>;
+    constexpr bool kPair = C::kPair;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     ProductControl *ctl = reinterpret_cast<ProductControl *>(ring + C::kStages * C::kStageBytes + C::kOutBytes);
@@ -592,7 +601,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     if (P.E <= kPrThreads - 1) {
         const int e = (int)threadIdx.x;
         const int o = ld_chained(P.offsets + min(e, P.E)), next = ld_chained(P.offsets + min(e + 1, P.E));
-        int t = e < P.E ? (next - o + kPrRows - 1) / kPrRows : 0;
+        int t = e < P.E ? (next - o + C::kRows - 1) / C::kRows : 0;
         const int own = t;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -609,26 +618,26 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             for (int w = 0; w < warp; ++w) base += ctl->warp_tiles[w];
             if (e <= P.E) ctl->tiles[e] = base + t - own;
         } else if (!fine && warp == 3) {
-            repair_offsets(P, ctl, lane);
+            repair_offsets(P, ctl, lane, C::kRows);
         }
     } else {
         for (int e = threadIdx.x; e <= P.E; e += kPrThreads) ctl->first[e] = ld_chained(P.offsets + e);
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-        if (warp == 3) repair_offsets(P, ctl, lane);
+        if (warp == 3) repair_offsets(P, ctl, lane, C::kRows);
     }
     __syncthreads();
     if (kPair) cluster_sync_all();     // the other CTA's barriers exist before anything arrives on them
     const uint32_t tmem_base = ctl->tmem_base;
     const int total = ctl->tiles[P.E] * P.NT;
     const unsigned long long deadline = globaltimer_ns() + P.wait_ns;
-    ProductWalk<kPair> walk(P, ctl);
+    ProductWalk<kKind> walk(P, ctl);
 
-    if (warp == 0) product_loader<kPair, kLoadW>(P, ctl, walk, total, deadline, rank, ring);
-    else if (warp == 2) product_loader<kPair, kLoadX>(P, ctl, walk, total, deadline, rank, ring);
-    else if (warp == 3) product_loader<kPair, kLoadWs>(P, ctl, walk, total, deadline, rank, ring);
-    else if (warp == 4 + kPrEpiWarps) product_loader<kPair, kLoadXs>(P, ctl, walk, total, deadline, rank, ring);
+    if (warp == 0) product_loader<kKind, kLoadW>(P, ctl, walk, total, deadline, rank, ring);
+    else if (warp == 2) product_loader<kKind, kLoadX>(P, ctl, walk, total, deadline, rank, ring);
+    else if (warp == 3) product_loader<kKind, kLoadWs>(P, ctl, walk, total, deadline, rank, ring);
+    else if (warp == 4 + kPrEpiWarps) product_loader<kKind, kLoadXs>(P, ctl, walk, total, deadline, rank, ring);
     else if (warp == 1 && rank == 0) {
         // The whole warp runs the loop, converged, and one elected lane issues: warp-uniform operands, addresses that advance by additions,
         // the next stage's barrier looked at before this one's MMAs are issued.  The thread that issues paces the tensor pipe: with a
@@ -637,7 +646,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         constexpr uint32_t kLoStage = (uint32_t)(C::kStageBytes >> 4), kLoX = (uint32_t)(kPrWBytes >> 4), kLoWs = (uint32_t)((kPrWBytes + C::kXBytes) >> 4),
                            kLoXs = kLoWs + (uint32_t)(kPrWScaleBytes >> 4);
         const uint32_t lo0 = smem_desc_lo(smem_u32(ring)), full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
-        const uint32_t sw0 = tmem_base + (uint32_t)(2 * kPrRows);
+        const uint32_t sw0 = tmem_base + (uint32_t)(2 * C::kRows);
         uint32_t w_lo = lo0, full_bar = full0, empty_bar = empty0, sw = sw0, phase = 0;
         int it = 0;
         bool ok = true, ready = mbar_test_wait(full0, 0u);
@@ -674,7 +683,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
                 ok = __all_sync(0xffffffffu, pr_wait(smem_u32(&ctl->tmem_empty[a]), parity, ctl, deadline, P.status, (uint32_t)walk.g, 75u));
                 if (!ok) break;
             }
-            const uint32_t d_tmem = tmem_base + (uint32_t)(a * kPrRows);
+            const uint32_t d_tmem = tmem_base + (uint32_t)(a * C::kRows);
             uint32_t accumulate = 0u;
             for (int kb = 1; kb < P.num_kb; ++kb) {
                 wait_stage();
@@ -728,7 +737,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
                 asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %0, 0;\n\tbar.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "+r"(ok) : "r"(1 + unit) : "memory");
             if (!ok) break;
             tc_fence_after();
-            const uint32_t taddr = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(a * kPrRows);
+            const uint32_t taddr = tmem_base + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(a * C::kRows);
             const auto release = [&]() {
                 tc_fence_before();
                 __syncwarp();
@@ -778,9 +787,9 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     }
 }
 
-template <bool kPair>
-constexpr size_t pr_smem_bytes() { return (size_t)PrCfg<kPair>::kStages * PrCfg<kPair>::kStageBytes + PrCfg<kPair>::kOutBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127); }
-static_assert(pr_smem_bytes<false>() <= 227 * 1024 && pr_smem_bytes<true>() <= 227 * 1024, "the product's stages exceed the shared memory of an SM");
+template <int kKind>
+constexpr size_t pr_smem_bytes() { return (size_t)PrCfg<kKind>::kStages * PrCfg<kKind>::kStageBytes + PrCfg<kKind>::kOutBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127); }
+static_assert(pr_smem_bytes<kOneTiles>() <= 227 * 1024 && pr_smem_bytes<kPairTiles>() <= 227 * 1024 && pr_smem_bytes<kFewTiles>() <= 227 * 1024, "the product's stages exceed the shared memory of an SM");
 
 // Mean rows per expert from which tiles by pairs of CTAs pay: they read less per product, but there are half as many places for them.
 // One CTA / pair, us, skewed routing, at 80 / 136 / 181 to 200 / 248 to 300 / 409 to 546 / 992 or more rows per expert:
@@ -788,6 +797,12 @@ static_assert(pr_smem_bytes<false>() <= 227 * 1024 && pr_smem_bytes<true>() <= 2
 //   N 2048, K 1408   28.7/28.9  29.6/29.6  35.6/35.1  43.1/41.6  73.2/66.0  134/120
 //   N 1024, K 1536   12.4/13.4  14.5/15.3  17.5/18.5  19.8/20.5  22.8/22.7  62.8/59.8
 constexpr int32_t kPairRowsPerExpert = 256;
+// ... and up to which tiles of 64 rows in eight stages pay: 168 KB on their way to an SM instead of 105, but an expert of 65 rows reads its
+// weights twice.  192 / 64 rows, us, at 1 / 4 to 6 / 7 to 8 / 15 to 17 / 48 rows per expert:
+//   N 2816, K 2048   22.8/21.9  34.2/33.8  35.9/36.4  36.9/37.6  40.5/42.2
+//   N 2048, K 1408   16.4/15.4  20.8/19.2  22.5/21.0  23.8/22.2  25.8/24.7
+//   N 1024, K 1536    9.4/9.3   11.3/10.9  12.0/11.6  12.2/11.9  12.7/12.3
+constexpr int32_t kFewRowsPerExpert = 16;
 
 bool columns_ok(int32_t K) { return K >= kMxBlock && K % kMxBlock == 0 && K <= 1 << 20; }
 int64_t scale_blocks(int64_t rows, int32_t groups) { return rows / kMxTile + groups; }
@@ -834,18 +849,17 @@ int32_t describe(moe_handle *h, const char *who, int32_t rows, int32_t src_rows,
 
 using namespace moe;
 
-template <class E, bool kPair>
+template <int kKind>
 static cudaError_t prepare_product()
 {
-    return cudaFuncSetAttribute(mxfp4_product_kernel<E, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pr_smem_bytes<kPair>());
+    const cudaError_t e = cudaFuncSetAttribute(mxfp4_product_kernel<__nv_bfloat16, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pr_smem_bytes<kKind>());
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(mxfp4_product_kernel<__half, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pr_smem_bytes<kKind>());
 }
 cudaError_t moe::mxfp4_prepare()
 {
-    cudaError_t e = prepare_product<__nv_bfloat16, false>();
-    if (e == cudaSuccess) e = prepare_product<__half, false>();
-    if (e == cudaSuccess) e = prepare_product<__nv_bfloat16, true>();
-    if (e == cudaSuccess) e = prepare_product<__half, true>();
-    return e;
+    cudaError_t e = prepare_product<kOneTiles>();
+    if (e == cudaSuccess) e = prepare_product<kPairTiles>();
+    return e != cudaSuccess ? e : prepare_product<kFewTiles>();
 }
 
 extern "C" int32_t moe_mxfp4_scale_bytes(int32_t rows, int32_t K, int32_t groups, size_t *bytes)
@@ -916,18 +930,19 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     p.KQ = (K + kMxTile - 1) / kMxTile;
     p.num_kb = (K + kPrK - 1) / kPrK;
     p.last_steps = (K - (p.num_kb - 1) * kPrK + kPrStepK - 1) / kPrStepK;
-    const bool pair = h->max_pairs > 0 && N > kPrN && rows / E_tot >= kPairRowsPerExpert;
-    const int32_t tile_n = pair ? PrCfg<true>::kTileN : PrCfg<false>::kTileN;
+    const int kind = h->max_pairs > 0 && N > kPrN && rows / E_tot >= kPairRowsPerExpert ? kPairTiles : rows / E_tot <= kFewRowsPerExpert ? kFewTiles : kOneTiles;
+    const bool pair = kind == kPairTiles, few = kind == kFewTiles;
+    const int32_t tile_n = pair ? PrCfg<kPairTiles>::kTileN : kPrN, tile_rows = few ? PrCfg<kFewTiles>::kRows : PrCfg<kOneTiles>::kRows;
     p.NT = (N + tile_n - 1) / tile_n;
     p.by_NT = divisor_of(p.NT);
-    const int64_t used = rows < E_tot ? rows : E_tot, tiles = ((rows - used) / kPrRows + used) * p.NT;      // at most
+    const int64_t used = rows < E_tot ? rows : E_tot, tiles = ((rows - used) / tile_rows + used) * p.NT;    // at most
     if (tiles >= (int64_t)1 << 31) return MOE_ERR_SHAPE;
-    const int32_t boxes[3] = {pair ? PrCfg<true>::kXRows : PrCfg<false>::kXRows, pair ? 32 : 64, 16};
-    for (int i = 0; i < (pair ? 2 : 3); ++i)
-        if (!code_map(h, &p.tmX[i], x_codes, 0, rows, K / 2, boxes[i], "x_codes")) return MOE_ERR_CUDA;
+    const int32_t boxes[3][3] = {{PrCfg<kOneTiles>::kXRows, 64, 16}, {PrCfg<kPairTiles>::kXRows, 32, 0}, {PrCfg<kFewTiles>::kXRows, 16, 0}};
+    for (int i = 0; i < 3 && boxes[kind][i]; ++i)
+        if (!code_map(h, &p.tmX[i], x_codes, 0, rows, K / 2, boxes[kind][i], "x_codes")) return MOE_ERR_CUDA;
     if (pair && !out_map(h, &p.tmOut, out, rows, N, ld_out, kPrOutCols, kPrOutRows, "out")) return MOE_ERR_CUDA;
     if (!code_map(h, &p.tmW, w_codes, E_tot, N, K / 2, kPrN, "w_codes") ||
-        !scale_map(h, &p.tmXs, x_scales, scale_blocks(rows, E_tot), p.KQ, 2, "x_scales") ||
+        !scale_map(h, &p.tmXs, x_scales, scale_blocks(rows, E_tot), p.KQ, few ? 1 : 2, "x_scales") ||
         !scale_map(h, &p.tmWs, w_scales, scale_blocks((int64_t)E_tot * N, E_tot), p.KQ, 1, "w_scales"))
         return MOE_ERR_CUDA;
     const int64_t slots = pair ? h->max_pairs : h->G, grid = tiles < slots ? tiles : slots;
@@ -942,9 +957,11 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     cfg.stream = static_cast<cudaStream_t>(stream);
     cfg.gridDim = dim3((unsigned)(pair ? 2 * grid : grid));
     cfg.blockDim = dim3(kPrThreads);
-    cfg.dynamicSmemBytes = pair ? pr_smem_bytes<true>() : pr_smem_bytes<false>();
+    cfg.dynamicSmemBytes = pair ? pr_smem_bytes<kPairTiles>() : few ? pr_smem_bytes<kFewTiles>() : pr_smem_bytes<kOneTiles>();
     const bool half = dtype == MOE_FP16;
-    const cudaError_t err = pair ? cudaLaunchKernelEx(&cfg, half ? mxfp4_product_kernel<__half, true> : mxfp4_product_kernel<__nv_bfloat16, true>, p)
-                                 : cudaLaunchKernelEx(&cfg, half ? mxfp4_product_kernel<__half, false> : mxfp4_product_kernel<__nv_bfloat16, false>, p);
+    const auto launch = [&](auto one, auto two, auto three) { return cudaLaunchKernelEx(&cfg, pair ? two : few ? three : one, p); };
+    const cudaError_t err =
+        half ? launch(mxfp4_product_kernel<__half, kOneTiles>, mxfp4_product_kernel<__half, kPairTiles>, mxfp4_product_kernel<__half, kFewTiles>)
+             : launch(mxfp4_product_kernel<__nv_bfloat16, kOneTiles>, mxfp4_product_kernel<__nv_bfloat16, kPairTiles>, mxfp4_product_kernel<__nv_bfloat16, kFewTiles>);
     return err == cudaSuccess ? MOE_OK : cuda_fail(h, err, "grouped 4-bit product launch");
 }

@@ -446,6 +446,19 @@ def test_product_at_row_counts_around_the_steps(M):
     check_product(out, xv, wv, offsets, K, torch.bfloat16)
 
 
+@pytest.mark.parametrize("M", [1, 15, 16, 17, 31, 33, 48, 63, 64, 65, 127, 128, 129, 192, 200])
+def test_few_rows_an_expert_with_one_that_has_more(M):
+    # tiles of 64 rows in more stages: the longest sequences of stages (K = 2720: eleven), more than one tile for an expert
+    E, N, K = 20, 264, 2720
+    offsets = [0] * 3 + [5] + [5 + M] * 8 + [6 + M] * 9
+    assert len(offsets) == E + 1 and offsets[-1] // E <= 16
+    xc, xs, wc, ws, xv, wv = product_case(offsets, offsets[-1], N, K, M)
+    out, st = torch.empty((offsets[-1], N), dtype=torch.bfloat16, device="cuda"), status()
+    B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, ints(offsets), out, st)
+    assert st.tolist() == [0, 0, 0, 0]
+    check_product(out, xv, wv, offsets, K, torch.bfloat16)
+
+
 @pytest.mark.parametrize("M", [1, 15, 17, 31, 32, 33, 63, 64, 65, 96, 97, 128, 129, 191, 192, 193, 256, 257, 320, 321, 385])
 @pytest.mark.parametrize("N, K", [(264, 384), (384, 1504)])
 def test_wide_tiles_at_row_counts_around_the_steps(M, N, K):
