@@ -791,13 +791,14 @@ template <int kKind>
 constexpr size_t pr_smem_bytes() { return (size_t)PrCfg<kKind>::kStages * PrCfg<kKind>::kStageBytes + PrCfg<kKind>::kOutBytes + 1024 + ((sizeof(ProductControl) + 127) & ~(size_t)127); }
 static_assert(pr_smem_bytes<kOneTiles>() <= 227 * 1024 && pr_smem_bytes<kPairTiles>() <= 227 * 1024 && pr_smem_bytes<kFewTiles>() <= 227 * 1024, "the product's stages exceed the shared memory of an SM");
 
-// Mean rows per expert from which tiles by pairs of CTAs pay: they read less per product, but there are half as many places for them.
-// One CTA / pair, us, skewed routing, at 80 / 136 / 181 to 200 / 248 to 300 / 409 to 546 / 992 or more rows per expert:
-//   N 2816, K 2048   44.5/45.1  44.3/44.1  58.3/56.7  70.2/66.7  118/109  214/196
-//   N 2048, K 1408   28.7/28.9  29.6/29.6  35.6/35.1  43.1/41.6  73.2/66.0  134/120
-//   N 1024, K 1536   12.4/13.4  14.5/15.3  17.5/18.5  19.8/20.5  22.8/22.7  62.8/59.8
-constexpr int32_t kPairRowsPerExpert = 256;
-// ... and up to which tiles of 64 rows in eight stages pay: 168 KB on their way to an SM instead of 105, but an expert of 65 rows reads its
+// Tiles by pairs of CTAs read less per product, but there are half as many places for them.  They pay from this many rows per expert
+// on, where every pair then has this many tiles.  One CTA / pair, us, skewed routing, at the rows per expert (tiles a pair) given:
+//   N 2816, K 2048   84 (14) 44.4/45.0   121 (17) 48.7/48.1   157 (18) 53.4/52.1   181 (19) 57.5/55.2   248 (22) 69.2/64.4   992 (61) 210/183
+//   N 2048, K 1408  100 (10) 26.3/26.9   136 (11) 29.8/29.8   157 (13) 35.3/33.9   181 (14) 36.1/35.0   248 (16) 42.9/40.9   992 (44) 132/113
+//   N 1536, K 512   200 (6) 14.4/15.0    300 (8) 17.5/18.6    409 (10) 20.6/21.5   520 (12) 22.7/23.4   819 (17) 30.8/30.8   1638 (31) 52.0/49.5
+//   N 1024, K 1536  200 (4) 17.5/18.5    300 (6) 20.5/20.7    409 (7) 23.2/22.8    819 (11) 35.7/34.0   1638 (20) 62.7/56.5
+constexpr int32_t kPairRowsPerExpert = 128, kPairTilesEach = 11;
+// Mean rows per expert up to which tiles of 64 rows in eight stages pay: 168 KB on their way to an SM instead of 105, but an expert of 65 rows reads its
 // weights twice.  192 / 64 rows, us, at 1 / 4 to 6 / 7 to 8 / 15 to 17 / 48 rows per expert:
 //   N 2816, K 2048   22.8/21.9  34.2/33.8  35.9/36.4  36.9/37.6  40.5/42.2
 //   N 2048, K 1408   16.4/15.4  20.8/19.2  22.5/21.0  23.8/22.2  25.8/24.7
@@ -930,12 +931,16 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     p.KQ = (K + kMxTile - 1) / kMxTile;
     p.num_kb = (K + kPrK - 1) / kPrK;
     p.last_steps = (K - (p.num_kb - 1) * kPrK + kPrStepK - 1) / kPrStepK;
-    const int kind = h->max_pairs > 0 && N > kPrN && rows / E_tot >= kPairRowsPerExpert ? kPairTiles : rows / E_tot <= kFewRowsPerExpert ? kFewTiles : kOneTiles;
+    const int64_t used = rows < E_tot ? rows : E_tot;
+    const auto tiles_at_most = [&](int tile_rows, int columns) { return ((rows - used) / tile_rows + used) * ((N + columns - 1) / columns); };
+    const bool pairs_pay = rows / E_tot >= kPairRowsPerExpert &&
+                           tiles_at_most(PrCfg<kPairTiles>::kRows, PrCfg<kPairTiles>::kTileN) >= (int64_t)kPairTilesEach * h->max_pairs;
+    const int kind = h->max_pairs > 0 && pairs_pay ? kPairTiles : rows / E_tot <= kFewRowsPerExpert ? kFewTiles : kOneTiles;
     const bool pair = kind == kPairTiles, few = kind == kFewTiles;
     const int32_t tile_n = pair ? PrCfg<kPairTiles>::kTileN : kPrN, tile_rows = few ? PrCfg<kFewTiles>::kRows : PrCfg<kOneTiles>::kRows;
     p.NT = (N + tile_n - 1) / tile_n;
     p.by_NT = divisor_of(p.NT);
-    const int64_t used = rows < E_tot ? rows : E_tot, tiles = ((rows - used) / tile_rows + used) * p.NT;    // at most
+    const int64_t tiles = tiles_at_most(tile_rows, tile_n);
     if (tiles >= (int64_t)1 << 31) return MOE_ERR_SHAPE;
     const int32_t boxes[3][3] = {{PrCfg<kOneTiles>::kXRows, 64, 16}, {PrCfg<kPairTiles>::kXRows, 32, 0}, {PrCfg<kFewTiles>::kXRows, 16, 0}};
     for (int i = 0; i < 3 && boxes[kind][i]; ++i)

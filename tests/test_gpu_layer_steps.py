@@ -459,16 +459,60 @@ def test_few_rows_an_expert_with_one_that_has_more(M):
     check_product(out, xv, wv, offsets, K, torch.bfloat16)
 
 
+# Tiles of 256 columns by two CTAs are for many rows an expert and many tiles: tests of them have many columns, and take their reference
+# on the GPU, in 64 bits from the values that the quantisation (tested above) left.
+WIDE_N = 29960                                          # 117 tiles of 256 columns and one of 8; with seven tiles of rows, eleven for each of 74 pairs
+
+
+def wide_case(offsets, x, w, E):
+    rows, K = x.shape
+    xc, xs, st1 = quantized(x.cuda(), E, ints(offsets))
+    wc, ws, st2 = quantized(w.cuda(), E)
+    xv, wv = torch.zeros((rows, K), device="cuda"), torch.empty((w.shape[0], K), device="cuda")
+    B.moe_mxfp4_dequantize(handle(), xc, xs, E, xv, st1, offsets=ints(offsets))
+    B.moe_mxfp4_dequantize(handle(), wc, ws, E, wv, st2)
+    return xc, xs, wc.reshape(E, -1, K // 2), ws, xv.double(), wv.double().reshape(E, -1, K)
+
+
+def check_wide(out, xv, wv, offsets, K):
+    eps = torch.finfo(out.dtype).eps / 2
+    for e in range(len(offsets) - 1):
+        x, got = xv[offsets[e]:offsets[e + 1]], out[offsets[e]:offsets[e + 1]].double()
+        want, mag = x @ wv[e].t(), x.abs() @ wv[e].abs().t()
+        assert ((got - want).abs() <= eps * want.abs() + TINY[out.dtype] / 2 + K * 2.0 ** -23 * mag).all(), e
+
+
 @pytest.mark.parametrize("M", [1, 15, 17, 31, 32, 33, 63, 64, 65, 96, 97, 128, 129, 191, 192, 193, 256, 257, 320, 321, 385])
-@pytest.mark.parametrize("N, K", [(264, 384), (384, 1504)])
-def test_wide_tiles_at_row_counts_around_the_steps(M, N, K):
-    # many rows an expert on average: tiles of 256 columns by two CTAs
-    offsets = [0, 300, 300 + M, 800 + M]
-    xc, xs, wc, ws, xv, wv = product_case(offsets, 800 + M, N, K, M)
-    out, st = torch.empty((800 + M, N), dtype=torch.bfloat16, device="cuda"), status()
+@pytest.mark.parametrize("K, dtype", [(384, torch.bfloat16), (1504, torch.float16)])
+def test_wide_tiles_at_row_counts_around_the_steps(M, K, dtype):
+    offsets, E = [0, 300, 300 + M, 800 + M], 3
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x, w = torch.randn((800 + M, K), device="cuda", generator=g), 0.05 * torch.randn((E * WIDE_N, K), device="cuda", generator=g)
+    xc, xs, wc, ws, xv, wv = wide_case(offsets, x, w, E)
+    out, st = pitched(torch.full((803 + M, WIDE_N), 7.0, dtype=dtype), WIDE_N + 8)[:800 + M], status()
     B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, ints(offsets), out, st)
     assert st.tolist() == [0, 0, 0, 0]
-    check_product(out, xv, wv, offsets, K, torch.bfloat16)
+    check_wide(out, xv, wv, offsets, K)
+    assert torch.isnan(out.as_strided((799 + M, 8), (WIDE_N + 8, 1), WIDE_N)).all()      # between the rows
+    assert (out.as_strided((3, WIDE_N), (WIDE_N + 8, 1), (800 + M) * (WIDE_N + 8)) == 7.0).all()      # behind them
+
+
+def test_wide_tiles_with_exponents_far_apart_and_no_numbers():
+    offsets, K, E = [0, 250, 1100], 512, 2
+    g = torch.Generator(device="cuda").manual_seed(1)
+    far = lambda n: torch.randn((n, K // 32, 32), device="cuda", generator=g) * torch.exp2(torch.randint(-30, 30, (n, K // 32, 1), device="cuda", generator=g).float())  # noqa: E731
+    x, w = far(1100).reshape(1100, K), far(E * WIDE_N).reshape(E * WIDE_N, K)
+    xc, xs, wc, ws, xv, wv = wide_case(offsets, x, w, E)
+    out, st = torch.empty((1100, WIDE_N), dtype=torch.bfloat16, device="cuda"), status()
+    B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, ints(offsets), out, st)
+    check_wide(out, xv, wv, offsets, K)
+    x[300, 40], w[5, 200] = float("nan"), float("inf")  # expert 1; expert 0, column 5
+    xc, xs, wc, ws, _, _ = wide_case(offsets, x, w, E)
+    hurt = torch.empty_like(out)
+    B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, ints(offsets), hurt, st)
+    bad = torch.isnan(hurt)
+    assert bad[300].all() and bad[:250, 5].all() and int(bad.sum()) == WIDE_N + 250
+    assert torch.equal(hurt[~bad], out[~bad]) and st.tolist() == [0, 0, 0, 0]
 
 
 @pytest.mark.parametrize("offsets, rows", [([0, 150, 300], 300), ([0, 250, 600], 600)])
@@ -846,8 +890,9 @@ def test_products_on_two_streams_at_once():
     # both families of tiles beside each other and beside the row kernels, against the same calls one after the other
     small, large = [0, 5, 9, 30], [0, 400, 401, 900]
     jobs = []
-    for offsets, N, K, seed in ((small, 264, 320, 1), (large, 264, 320, 2)):
-        xc, xs, wc, ws, _, _ = product_case(offsets, offsets[-1], N, K, seed)
+    for offsets, N, K, seed in ((small, 264, 320, 1), (large, WIDE_N, 320, 2)):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        xc, xs, wc, ws, _, _ = wide_case(offsets, torch.randn((offsets[-1], K), device="cuda", generator=g), torch.randn((3 * N, K), device="cuda", generator=g), 3)
         jobs.append((xc, xs, wc, ws, ints(offsets), [torch.zeros((offsets[-1], N), dtype=torch.bfloat16, device="cuda") for _ in range(2)], status(), torch.cuda.Stream()))
     torch.cuda.synchronize()
     for which in range(2):
