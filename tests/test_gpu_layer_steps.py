@@ -585,8 +585,8 @@ def test_product_past_32_bits():
 
 
 def test_product_of_many_experts_past_32_bits():
-    R, N, K, E = 255000, 8456, 32, 1000                 # 2.16e9 elements out, 255 rows an expert
-    offsets = ints([255 * e for e in range(E + 1)])
+    R, N, K, E = 127000, 16960, 32, 1000                # 2.15e9 elements out, 127 rows an expert: tiles of one CTA
+    offsets = ints([127 * e for e in range(E + 1)])
     codes = torch.randint(0, 256, (R, K // 2), dtype=torch.uint8, device="cuda")
     xs = torch.full((B.moe_mxfp4_scale_bytes(R, K, E),), 127, dtype=torch.uint8, device="cuda")
     wc = torch.randint(0, 256, (E, N, K // 2), dtype=torch.uint8, device="cuda")
@@ -594,7 +594,7 @@ def test_product_of_many_experts_past_32_bits():
     out, st = torch.empty((R, N), dtype=torch.bfloat16, device="cuda"), status()
     B.moe_mxfp4_gemm(handle(), codes, xs, wc, ws, offsets, out, st)
     for e in (0, 500, 999):
-        at = 255 * e + 250
+        at = 127 * e + 122
         x = ref.dequantize(codes[at:at + 5].cpu().numpy(), np.full((5, 1), 127, np.uint8))
         want = x @ ref.dequantize(wc[e].cpu().numpy(), np.full((N, 1), 127, np.uint8)).T     # multiples of 1/4 below 2^11: exact in fp32
         assert (np.abs(f64(out[at:at + 5]) - want) <= half_step(torch.bfloat16, want)).all()
