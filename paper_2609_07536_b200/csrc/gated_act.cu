@@ -27,11 +27,23 @@ struct GatedAct {
     Divisor by_lanes;
 };
 
+// x / (1 + exp(-g)), down to fp32's smallest numbers: at g = -88.7, where exp(-g) leaves the range of fp32, silu(g) is -3e-37, a normal
+// number, and another factor may make it an ordinary one.  fp32: of exp(-|g|), which is at most 1.  16-bit results do not see the
+// approximations' last bits: 2^-24 / (2^-24 + 2^(-24 - g log2(e))), whose exponential ends where the quotient does, at 2^150, and costs no
+// instruction more.  Absolute error of the quotient where it is subnormal: a step of 2^-149.
 template <class E>
-__device__ __forceinline__ float exp_of(float x) { return sizeof(E) == 4 ? expf(x) : __expf(x); }
-// a / b; 16-bit results do not see the approximation's last bits (nor values below 2^-118, which it takes for zero)
-template <class E>
-__device__ __forceinline__ float ratio(float a, float b) { return sizeof(E) == 4 ? a / b : __fdividef(a, b); }
+__device__ __forceinline__ float sigmoid_times(float x, float g)
+{
+    if constexpr (sizeof(E) == 4) {
+        const float e = expf(-fabsf(g));
+        return (g < 0.0f ? x * e : x) / (1.0f + e);
+    } else {
+        float e, r;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(-g, 1.44269504f, -24.0f)));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(0x1p-24f + e));
+        return x * (r * 0x1p-24f);
+    }
+}
 
 // sixteen codes of x * 2^-e, x = 0 .. 448 * 2^e in magnitude
 __device__ __forceinline__ uint4 e4m3_codes(const float (&x)[16], int e)
@@ -82,8 +94,8 @@ __device__ __forceinline__ void e4m3_values(uint2 c, float scale, float (&x)[8])
 
 // Two threads share the exponents of 32 columns.  What costs besides the bytes is the issue of the instructions that make the copy: a
 // thread takes 16 columns, so that addresses and exponents are worked out once for them, and finds its largest magnitudes in the
-// 16-bit patterns, two values a step.  131072 rows of 2 x 1408 in bf16: 232 us, 98 % of the measured copy bandwidth (8 columns a thread and
-// magnitudes in fp32: 304); without the copy 164 us.
+// 16-bit patterns, two values a step.  131072 rows of 2 x 1408 in bf16: 226 us, 101 % of the measured copy bandwidth (8 columns a thread and
+// magnitudes in fp32: 304); without the copy 163 us.
 template <class E, bool kKeep>
 __global__ void __launch_bounds__(kActThreads, 4) gated_act_kernel(const __grid_constant__ GatedAct p, const E *gate_up, E *act)
 {
@@ -106,7 +118,7 @@ __global__ void __launch_bounds__(kActThreads, 4) gated_act_kernel(const __grid_
         const auto activate = [&]() {
             float y[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = ratio<E>(g[i], 1.0f + exp_of<E>(-g[i])) * u[i];
+            for (int i = 0; i < 16; ++i) y[i] = sigmoid_times<E>(g[i], g[i]) * u[i];
             store16<E>(act + row * p.ld_act + q * 16, p.wide, y);
         };
         if (!kKeep) {
@@ -149,7 +161,7 @@ __global__ void __launch_bounds__(kActThreads, 4) gated_act_kernel(const __grid_
     }
 }
 
-// 131072 rows of 2 x 1408 in bf16, the activation written again: 279 us, 1.86 GB at the measured copy bandwidth.
+// 131072 rows of 2 x 1408 in bf16, the activation written again: 280 us, 1.86 GB at the measured copy bandwidth.
 template <class E>
 __global__ void __launch_bounds__(kActThreads) gated_act_grad_kernel(const __grid_constant__ GatedAct p, const E *d_act, E *d_gate_up, E *act)
 {
@@ -169,7 +181,7 @@ __global__ void __launch_bounds__(kActThreads) gated_act_grad_kernel(const __gri
         e4m3_values(cu, su, u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float s = ratio<E>(1.0f, 1.0f + exp_of<E>(-g[i])), silu = g[i] * s;
+            const float s = sigmoid_times<E>(1.0f, g[i]), silu = g[i] * s;
             const float dg = d[i] * u[i] * (s * fmaf(g[i], 1.0f - s, 1.0f));
             u[i] *= silu;                   // act
             d[i] *= silu;                   // d_up
