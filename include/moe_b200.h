@@ -521,7 +521,8 @@ int32_t moe_mxfp4_dequantize(moe_handle *h, const void *codes, const void *scale
 /* out[r][n] = sum_k x[r][k] * w[e][n][k] for the rows r of expert e (offsets[e] <= r < offsets[e + 1]), one persistent tcgen05 launch.
  * x_codes [rows, K / 2] with x_scales in E_tot groups by `offsets` [device] int32 [E_tot + 1]; w_codes [E_tot, N, K / 2] with w_scales in E_tot
  * groups of N rows.  N % 8 == 0, E_tot <= 1024.  dtype of out [rows, N]: MOE_BF16 or MOE_FP16.  fp32 accumulation.  Rows from
- * offsets[E_tot] on stay as they are.  Offsets that go back or past `rows` are reported and the rows they name skipped. */
+ * offsets[E_tot] on stay as they are.  Offsets that go back or past `rows` are reported: an expert that one of them begins or ends, or
+ * that begins inside the rows of one before it, has no rows, and the others are computed as they are. */
 int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void *x_scales, const void *w_codes, const void *w_scales,
                        const int32_t *offsets, int32_t rows, int32_t E_tot, int32_t N, int32_t K, int32_t dtype, void *out,
                        int64_t ld_out, uint32_t *status_dev, void *stream);

@@ -261,7 +261,7 @@ struct ProductControl {
     uint32_t tmem_base;
     volatile uint32_t abort;
     int32_t warp_tiles[kPrThreads / 32];
-    int32_t first[kMaxExperts + 1];       // row where an expert's rows begin
+    int32_t first[kMaxExperts + 1];       // the offsets, as they are
     int32_t tiles[kMaxExperts + 1];       // row tiles of the experts before
 };
 
@@ -532,33 +532,32 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
-// Row tiles counted by one warp, whatever the offsets and however many: a running maximum, clamped to the rows
-__device__ __noinline__ void repair_offsets(const ProductParams &P, ProductControl *ctl, int lane, int tile_rows)
+// Row tiles counted by one warp, whatever the offsets and however many.  An expert has rows where its two offsets are in order and within
+// the rows, and where it begins behind the rows of all such experts before it; tiles of any other are never walked to.
+__device__ __noinline__ void count_tiles(const ProductParams &P, ProductControl *ctl, int lane, int tile_rows)
 {
-    int tiles = 0, before = 0;
+    int tiles = 0, top = 0;                      // of the experts before this round of 32: their tiles, where their rows end
     for (int e0 = 0; e0 <= P.E; e0 += 32) {
-        const int e = e0 + lane, raw = ctl->first[min(e, P.E)];
-        int o = min(max(raw, before), P.R);
+        const int e = e0 + lane, begin = ctl->first[min(e, P.E)], end = ctl->first[min(e + 1, P.E)];
+        const bool ordered = begin >= 0 && begin <= end && end <= P.R;
+        if (e <= P.E && !ordered && blockIdx.x == 0) report(P.status, MOE_DEV_OOB, (uint32_t)e, 63u);
+        int ends = ordered ? end : 0;            // running maximum of the ends up to this expert
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int u = __shfl_up_sync(0xffffffffu, o, d);
-            if (lane >= d) o = max(o, u);
+            const int u = __shfl_up_sync(0xffffffffu, ends, d);
+            if (lane >= d) ends = max(ends, u);
         }
-        if (e <= P.E && o != raw && blockIdx.x == 0) report(P.status, MOE_DEV_OOB, (uint32_t)e, 63u);
-        int prev = __shfl_up_sync(0xffffffffu, o, 1);
-        if (lane == 0) prev = before;
-        // row tiles of the expert that ends at `o` (expert e - 1)
-        int t = (e > 0 && e <= P.E) ? (o - prev + tile_rows - 1) / tile_rows : 0;
+        int before = __shfl_up_sync(0xffffffffu, ends, 1);
+        before = lane == 0 ? top : max(before, top);
+        const int own = e < P.E && ordered && begin >= before ? (end - begin + tile_rows - 1) / tile_rows : 0;
+        int t = own;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int u = __shfl_up_sync(0xffffffffu, t, d);
             if (lane >= d) t += u;
         }
-        if (e <= P.E) {
-            ctl->first[e] = o;
-            ctl->tiles[e] = tiles + t;
-        }
-        before = __shfl_sync(0xffffffffu, o, 31);
+        if (e <= P.E) ctl->tiles[e] = tiles + t - own;
+        top = max(top, __shfl_sync(0xffffffffu, ends, 31));
         tiles += __shfl_sync(0xffffffffu, t, 31);
     }
 }
@@ -597,11 +596,12 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     }
     grid_dependency_wait();
     // Where the experts' rows begin and how many row tiles lie before them.  A thread has an expert; offsets that go back or past the rows
-    // are reported, and what they name has no rows.
+    // are reported, and the experts beside them have no rows.
     if (P.E <= kPrThreads - 1) {
         const int e = (int)threadIdx.x;
         const int o = ld_chained(P.offsets + min(e, P.E)), next = ld_chained(P.offsets + min(e + 1, P.E));
-        int t = e < P.E ? (next - o + C::kRows - 1) / C::kRows : 0;
+        const bool ordered = o >= 0 && o <= next && next <= P.R;
+        int t = e < P.E && ordered ? (next - o + C::kRows - 1) / C::kRows : 0;
         const int own = t;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -611,21 +611,21 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         if (e <= P.E) ctl->first[e] = o;
         if (lane == 31) ctl->warp_tiles[warp] = t;
         tc_fence_before();
-        const bool fine = __syncthreads_and(o >= 0 && o <= next && next <= P.R) != 0;
+        const bool fine = __syncthreads_and(ordered) != 0;
         tc_fence_after();
         if (fine && 32 * warp <= P.E) {
             int base = 0;
             for (int w = 0; w < warp; ++w) base += ctl->warp_tiles[w];
             if (e <= P.E) ctl->tiles[e] = base + t - own;
         } else if (!fine && warp == 3) {
-            repair_offsets(P, ctl, lane, C::kRows);
+            count_tiles(P, ctl, lane, C::kRows);
         }
     } else {
         for (int e = threadIdx.x; e <= P.E; e += kPrThreads) ctl->first[e] = ld_chained(P.offsets + e);
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-        if (warp == 3) repair_offsets(P, ctl, lane, C::kRows);
+        if (warp == 3) count_tiles(P, ctl, lane, C::kRows);
     }
     __syncthreads();
     if (kPair) cluster_sync_all();     // the other CTA's barriers exist before anything arrives on them
