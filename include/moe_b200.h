@@ -507,7 +507,9 @@ int32_t moe_gated_act_grad(moe_handle *h, const void *d_act, int64_t ld_d_act, c
  *          (experts): row r of group g, whose rows begin at o, is row (r - o) % 128 of row block o / 128 + g + (r - o) / 128.
  *          Exponents of columns past K are written as 0 and have to be less than 255 in a buffer that another program fills.
  * Groups: offsets_or_null [device] int32 [groups + 1], from 0 up (routing.offsets; rows from the last entry on stay as
- * they are), or NULL: rows / groups rows each (weights [E, N, K] are rows E * N in E groups).
+ * they are), or NULL: rows / groups rows each (weights [E, N, K] are rows E * N in E groups).  Offsets that go back or past `rows` are
+ * reported: the rows of a group that one of them begins or ends, or that begins inside the rows of one before it, stay as they are
+ * (of more than 1024 groups, a row has its place by a bisection of the offsets, or none).
  * moe_mxfp4_quantize: src [rows, K].  With inv_perm_or_null [device] int32 [rows / copies, copies], src is [rows / copies, K] and row t is put
  * into rows inv_perm[t][0 ..] (-1: none): tokens are quantised once, into routed order.  Without it copies = 1.
  * moe_mxfp4_dequantize: out [rows, K] = codes times their powers of two. */

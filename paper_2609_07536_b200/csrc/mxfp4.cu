@@ -51,29 +51,25 @@ __device__ __forceinline__ void hold_offsets(const Quant &p, int32_t *held)
     if (p.offsets && p.groups <= kQuantGroupsHeld)
         for (int g = threadIdx.x; g <= p.groups; g += kQuantThreads) held[g] = ld_chained(p.offsets + g);
 }
+__device__ __forceinline__ bool ordered(const Quant &p, int begin, int end) { return begin >= 0 && begin <= end && end <= p.rows; }
+// All threads meet here; false: offsets that are not in order, or more than are held.  The last threads look them over, while the first
+// ones find their rows.
+__device__ __forceinline__ bool meet_with_offsets_ordered(const Quant &p, const int32_t *held)
+{
+    if (!p.offsets) {
+        __syncthreads();
+        return true;
+    }
+    bool fine = p.groups <= kQuantGroupsHeld;
+    if (fine)
+        for (int g = kQuantThreads - 1 - (int)threadIdx.x; g < p.groups; g += kQuantThreads) fine = fine && ordered(p, held[g], held[g + 1]);
+    return __syncthreads_and(fine) != 0;
+}
 
-// Where row `r` lies; rows behind the last group have no place
-__device__ __forceinline__ QuantRow quant_row(const Quant &p, const int32_t *held, int r, uint32_t what)
+// Row `r` of group `g`, whose rows begin at `o`
+__device__ __forceinline__ QuantRow row_in_group(const Quant &p, int r, int g, int o, uint32_t what)
 {
     QuantRow q = {nullptr, nullptr};
-    if (r < 0) return q;
-    int g, o;
-    if (p.offsets) {
-        const bool all = p.groups <= kQuantGroupsHeld;
-        const auto offset = [&](int i) { return all ? held[i] : ld_chained(p.offsets + i); };
-        if (r >= offset(p.groups)) return q;
-        int lo = 0, hi = p.groups - 1;         // the last group that begins at or before r: the one with rows among equals
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (offset(mid) <= r) lo = mid;
-            else hi = mid - 1;
-        }
-        g = lo;
-        o = offset(g);
-    } else {
-        g = quotient(p.by_n, r);
-        o = g * p.n_even;
-    }
     const int i = r - o;
     const long long block = (long long)(o / kMxTile) + g + i / kMxTile;
     if (o < 0 || i < 0 || block >= p.blocks) {
@@ -83,6 +79,64 @@ __device__ __forceinline__ QuantRow quant_row(const Quant &p, const int32_t *hel
     q.codes = p.codes + (long long)r * (p.K / 2);
     q.scales = p.scales + block * p.KQ * kMxTileBytes + (i & 31) * 16 + ((i & 127) >> 5) * 4;
     return q;
+}
+// the last group that begins at or before r: the one with rows among equals
+template <class Offset>
+__device__ __forceinline__ int bisect(const Quant &p, int r, Offset offset)
+{
+    int lo = 0, hi = p.groups - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (offset(mid) <= r) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+// Where row `r` lies, by offsets that are held and in order (of others, it has a place found again below); rows behind the last group have no place
+__device__ __forceinline__ QuantRow quant_row(const Quant &p, const int32_t *held, int r, uint32_t what)
+{
+    int g, o;
+    if (p.offsets) {
+        if (r < 0 || p.groups > kQuantGroupsHeld || r >= held[p.groups]) return {nullptr, nullptr};
+        g = bisect(p, r, [&](int i) { return held[i]; });
+        o = held[g];
+    } else {
+        if (r < 0) return {nullptr, nullptr};
+        g = quotient(p.by_n, r);
+        o = g * p.n_even;
+    }
+    return row_in_group(p, r, g, o, what);
+}
+// Where the rows of a block lie (row0: the first of the source; gather: by inv_perm) by offsets that are not in order, or more than are held.
+// A group has rows where its two offsets are in order and it begins behind the rows of all such groups before it, as in the product.  Of
+// more than are held, a row has the group that the bisection finds, where that and the offset before it are in order; the blocks look the
+// offsets over together.  Out of line, and the caller loads its columns again: inlined, or with them kept across the call, it took
+// registers that cost weights 5 of 70 us.
+__device__ __noinline__ void find_places_again(const Quant &p, const int32_t *held, QuantRow *where, int row0, int n, bool gather)
+{
+    const bool all = p.groups <= kQuantGroupsHeld;
+    const auto offset = [&](int i) { return all ? held[i] : ld_chained(p.offsets + i); };
+    if (!all || blockIdx.x == 0)
+        for (long long g = (long long)blockIdx.x * kQuantThreads + threadIdx.x; g < p.groups; g += (all ? 1ll : (long long)gridDim.x) * kQuantThreads)
+            if (!ordered(p, offset((int)g), offset((int)g + 1))) report(p.status, MOE_DEV_OOB, (uint32_t)g, 63u);
+    for (int k = threadIdx.x; k < n; k += kQuantThreads) {
+        const long long f = (long long)row0 * (gather ? p.copies : 1) + k;
+        const int r = gather ? ld_chained(p.inv_perm + f) : (int)f;
+        int found = -1;
+        if (!all && r >= 0 && r < p.rows) {
+            const int g = bisect(p, r, offset);
+            if (ordered(p, offset(g), offset(g + 1)) && r < offset(g + 1) && (g == 0 || offset(g - 1) <= offset(g))) found = g;
+        }
+        for (int g = 0, top = 0; all && g < p.groups; ++g) {
+            if (!ordered(p, held[g], held[g + 1])) continue;
+            if (held[g] >= top && held[g] <= r && r < held[g + 1]) found = g;
+            top = max(top, held[g + 1]);
+        }
+        QuantRow q = {nullptr, nullptr};
+        if (found >= 0) q = row_in_group(p, r, found, offset(found), (uint32_t)f);
+        where[k] = q;
+    }
+    __syncthreads();
 }
 
 // e2m1 codes of eight values times `inv`, the first in the lowest four bits
@@ -99,9 +153,9 @@ __device__ __forceinline__ uint32_t e2m1_codes(const float *x, float inv)
 // bytes, the issue of instructions costs: with 8 columns a thread, and magnitudes found in fp32 one by one, weights of 60 x 2048 x 1408
 // took 126 us, now 71 (6.2 TB/s).  A block's first columns, its rows' numbers and the groups' offsets are fetched side by side: one
 // behind the other they were most of what a small batch took, and of tokens into routed order, whose blocks are many and short (16384
-// tokens, 8 rows each: 52 us, now 42, of which the codes are 15, the exponents' scattered words 9).
+// tokens, 8 rows each: 52 us, now 43, of which the codes are 15, the exponents' scattered words 9).
 template <class E, bool kGather>
-__global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const __grid_constant__ Quant p, const E *src)
+__global__ void __launch_bounds__(kQuantThreads, sizeof(E) == 2 ? 8 : 6) quantize_kernel(const __grid_constant__ Quant p, const E *src)
 {
     __shared__ QuantRow where[kQuantEntriesMax];
     __shared__ int32_t held[kQuantGroupsHeld + 1];
@@ -132,7 +186,10 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const __grid_co
         }
         where[k] = quant_row(p, held, r, (uint32_t)f);
     }
-    __syncthreads();
+    if (!meet_with_offsets_ordered(p, held)) {
+        find_places_again(p, held, where, row0, n * p.copies, kGather);
+        fetch(tid);
+    }
     for (int base = tid & ~31; base < items; base += kQuantThreads) {
         const int it = base + (tid & 31);
         if (base >= kQuantThreads) fetch(it);
@@ -170,7 +227,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const __grid_
     hold_offsets(p, held);
     __syncthreads();
     if ((int)threadIdx.x < n) where[threadIdx.x] = quant_row(p, held, row0 + (int)threadIdx.x, (uint32_t)(row0 + (int)threadIdx.x));
-    __syncthreads();
+    if (!meet_with_offsets_ordered(p, held)) find_places_again(p, held, where, row0, n, false);
     const int items = n * p.lanes;
     for (int it = (int)threadIdx.x; it < items; it += kQuantThreads) {
         const int i = quotient(p.by_lanes, it), q = it - i * p.lanes;
