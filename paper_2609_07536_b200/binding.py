@@ -566,15 +566,21 @@ def _mxfp4_bytes(rows, K, groups):
 
 def moe_mxfp4_quantize(h, src, codes, scales, groups, status_dev, offsets=None, inv_perm=None, copies=None, stream=None):
     """src [rows, K] -> codes uint8 [rows, K / 2] and scales (moe_mxfp4_scale_bytes) in `groups` groups: by offsets int32
-    [groups + 1], or of equally many rows.  inv_perm int32 [T, copies], or its address with `copies`: src is [T, K], row t goes to the
-    rows inv_perm[t]."""
+    [groups + 1], or of equally many rows.  inv_perm int32 [T, copies], or flat or its address with `copies`: src is [T, K], row t goes
+    to the rows inv_perm[t]."""
     who, dev = "moe_mxfp4_quantize", _device()
     half, n = codes.shape[-1], codes.numel()
     rows, K = n // max(1, half), 2 * half
     if inv_perm is not None and not isinstance(inv_perm, int):
-        if inv_perm.numel() != rows or copies not in (None, inv_perm.shape[-1]):
-            raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm names {inv_perm.numel()} rows, codes have {rows}")
-        copies = inv_perm.shape[-1]
+        named = inv_perm.shape
+        if inv_perm.numel() != rows or len(named) > 2:
+            raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm {tuple(named)} is not [T, copies] of the {rows} rows that codes have")
+        if len(named) == 2:
+            if copies not in (None, named[1]):
+                raise MoeError(MOE_ERR_SHAPE, who, f"inv_perm has {named[1]} copies of a row, not {copies}")
+            copies = named[1]
+        elif copies is None or copies < 1 or rows % copies:
+            raise MoeError(MOE_ERR_SHAPE, who, f"a flat inv_perm of {rows} rows needs the number of copies, not {copies}")
     copies = max(1, copies or 1)
     kind = src.dtype
     a, lda = _matrix(src, rows // copies, K, kind, dev, who, "src")
