@@ -528,6 +528,9 @@ int32_t moe_mxfp4_dequantize(moe_handle *h, const void *codes, const void *scale
 int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void *x_scales, const void *w_codes, const void *w_scales,
                        const int32_t *offsets, int32_t rows, int32_t E_tot, int32_t N, int32_t K, int32_t dtype, void *out,
                        int64_t ld_out, uint32_t *status_dev, void *stream);
+/* The tiles that the product is divided into at these sizes, as moe_select_tile says it of the fused calls: tile_rows rows of x by tile_cols
+ * columns of out.  (192, 256) by pairs of CTAs where experts have many rows, (64, 128) where they have few, (192, 128) else.  [host] */
+int32_t moe_mxfp4_select_tile(moe_handle *h, int32_t rows, int32_t E_tot, int32_t N, int32_t *tile_rows, int32_t *tile_cols);
 
 #ifdef __cplusplus
 }

@@ -39,6 +39,7 @@ EXPORTS = [
     "moe_select_tile", "moe_release_workspace", "moe_set_probe",
     "moe_permute", "moe_permute_grad", "moe_unpermute", "moe_unpermute_grad", "moe_gated_act", "moe_gated_act_grad",
     "moe_mxfp4_scale_bytes", "moe_mxfp4_quantize", "moe_mxfp4_dequantize", "moe_mxfp4_gemm",
+    "moe_mxfp4_select_tile",
 ]
 
 
@@ -159,6 +160,7 @@ def lib():
         L.moe_mxfp4_quantize.argtypes = [vp, vp, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp]
         L.moe_mxfp4_dequantize.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, i64, vp, vp]
         L.moe_mxfp4_gemm.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp, vp]
+        L.moe_mxfp4_select_tile.argtypes = [vp, i32, i32, i32, P(i32), P(i32)]
         for name in EXPORTS:
             if name != "moe_last_cuda_error":
                 getattr(L, name).restype = i32
@@ -616,6 +618,13 @@ def moe_mxfp4_gemm(h, x_codes, x_scales, w_codes, w_scales, offsets, out, status
         _vector(w_codes, 0, _u8, dev, who, "w_codes"), _vector(w_scales, _mxfp4_bytes(E * N, K, E), _u8, dev, who, "w_scales"),
         _vector(offsets, E + 1, _i32, dev, who, "offsets"), rows, E, N, K, _row_type(kind, who), a, lda, _vector(status_dev, 4, _i32, dev, who, "status_dev"),
         _raw_stream(stream, dev)), who, h)
+
+
+def moe_mxfp4_select_tile(h, rows: int, E_tot: int, N: int):
+    """(rows, columns) of the tiles that moe_mxfp4_gemm takes at these sizes."""
+    tr, tc = C.c_int32(), C.c_int32()
+    _check(lib().moe_mxfp4_select_tile(h, rows, E_tot, N, C.byref(tr), C.byref(tc)), "moe_mxfp4_select_tile", h)
+    return tr.value, tc.value
 
 
 # ----------------------------------------------------------------------------- device memory plumbing

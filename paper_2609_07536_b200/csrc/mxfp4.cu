@@ -862,6 +862,25 @@ constexpr int32_t kPairRowsPerExpert = 128, kPairTilesEach = 11;
 //   N 1024, K 1536    9.4/9.3   11.3/10.9  12.0/11.6  12.2/11.9  12.7/12.3
 constexpr int32_t kFewRowsPerExpert = 16;
 
+// tiles of a launch, whatever the offsets
+int64_t tiles_at_most(int32_t rows, int32_t E_tot, int32_t tile_rows, int32_t NT)
+{
+    const int64_t used = rows < E_tot ? rows : E_tot;
+    return ((rows - used) / tile_rows + used) * NT;
+}
+int product_kind(const moe_handle *h, int32_t rows, int32_t E_tot, int32_t N)
+{
+    using Pair = PrCfg<kPairTiles>;
+    if (h->max_pairs > 0 && rows / E_tot >= kPairRowsPerExpert &&
+        tiles_at_most(rows, E_tot, Pair::kRows, (N + Pair::kTileN - 1) / Pair::kTileN) >= (int64_t)kPairTilesEach * h->max_pairs)
+        return kPairTiles;
+    return rows / E_tot <= kFewRowsPerExpert ? kFewTiles : kOneTiles;
+}
+bool product_sizes_ok(int32_t rows, int32_t E_tot, int32_t N)
+{
+    return rows >= 0 && rows < 1 << 30 && E_tot >= 1 && E_tot <= kMaxExperts && N >= 8 && N % 8 == 0 && (int64_t)E_tot * N < 1 << 30;
+}
+
 bool columns_ok(int32_t K) { return K >= kMxBlock && K % kMxBlock == 0 && K <= 1 << 20; }
 int64_t scale_blocks(int64_t rows, int32_t groups) { return rows / kMxTile + groups; }
 
@@ -960,14 +979,22 @@ extern "C" int32_t moe_mxfp4_dequantize(moe_handle *h, const void *codes, const 
     });
 }
 
+extern "C" int32_t moe_mxfp4_select_tile(moe_handle *h, int32_t rows, int32_t E_tot, int32_t N, int32_t *tile_rows, int32_t *tile_cols)
+{
+    if (!h || !tile_rows || !tile_cols) return MOE_ERR_NULL;
+    if (!product_sizes_ok(rows, E_tot, N)) return MOE_ERR_SHAPE;
+    const int kind = product_kind(h, rows, E_tot, N);
+    *tile_rows = kind == kFewTiles ? PrCfg<kFewTiles>::kRows : PrCfg<kOneTiles>::kRows;
+    *tile_cols = kind == kPairTiles ? PrCfg<kPairTiles>::kTileN : kPrN;
+    return MOE_OK;
+}
+
 extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void *x_scales, const void *w_codes, const void *w_scales,
                                   const int32_t *offsets, int32_t rows, int32_t E_tot, int32_t N, int32_t K, int32_t dtype, void *out, int64_t ld_out,
                                   uint32_t *status_dev, void *stream)
 {
     if (!h || !status_dev) return MOE_ERR_NULL;
-    if (rows < 0 || rows >= 1 << 30 || E_tot < 1 || E_tot > kMaxExperts || N < 8 || N % 8 != 0 || (int64_t)E_tot * N >= 1 << 30 || !columns_ok(K) ||
-        !pitch_ok(ld_out, N))
-        return MOE_ERR_SHAPE;
+    if (!product_sizes_ok(rows, E_tot, N) || !columns_ok(K) || !pitch_ok(ld_out, N)) return MOE_ERR_SHAPE;
     if (dtype != MOE_BF16 && dtype != MOE_FP16) return MOE_ERR_UNSUPPORTED;
     if (rows == 0) return MOE_OK;
     if (!x_codes || !x_scales || !w_codes || !w_scales || !offsets || !out) return MOE_ERR_NULL;
@@ -988,16 +1015,12 @@ extern "C" int32_t moe_mxfp4_gemm(moe_handle *h, const void *x_codes, const void
     p.KQ = (K + kMxTile - 1) / kMxTile;
     p.num_kb = (K + kPrK - 1) / kPrK;
     p.last_steps = (K - (p.num_kb - 1) * kPrK + kPrStepK - 1) / kPrStepK;
-    const int64_t used = rows < E_tot ? rows : E_tot;
-    const auto tiles_at_most = [&](int tile_rows, int columns) { return ((rows - used) / tile_rows + used) * ((N + columns - 1) / columns); };
-    const bool pairs_pay = rows / E_tot >= kPairRowsPerExpert &&
-                           tiles_at_most(PrCfg<kPairTiles>::kRows, PrCfg<kPairTiles>::kTileN) >= (int64_t)kPairTilesEach * h->max_pairs;
-    const int kind = h->max_pairs > 0 && pairs_pay ? kPairTiles : rows / E_tot <= kFewRowsPerExpert ? kFewTiles : kOneTiles;
+    const int kind = product_kind(h, rows, E_tot, N);
     const bool pair = kind == kPairTiles, few = kind == kFewTiles;
     const int32_t tile_n = pair ? PrCfg<kPairTiles>::kTileN : kPrN, tile_rows = few ? PrCfg<kFewTiles>::kRows : PrCfg<kOneTiles>::kRows;
     p.NT = (N + tile_n - 1) / tile_n;
     p.by_NT = divisor_of(p.NT);
-    const int64_t tiles = tiles_at_most(tile_rows, tile_n);
+    const int64_t tiles = tiles_at_most(rows, E_tot, tile_rows, p.NT);
     if (tiles >= (int64_t)1 << 31) return MOE_ERR_SHAPE;
     const int32_t boxes[3][3] = {{PrCfg<kOneTiles>::kXRows, 64, 16}, {PrCfg<kPairTiles>::kXRows, 32, 0}, {PrCfg<kFewTiles>::kXRows, 16, 0}};
     for (int i = 0; i < 3 && boxes[kind][i]; ++i)

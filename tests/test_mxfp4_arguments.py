@@ -31,3 +31,9 @@ def test_a_flat_inv_perm_does_not_say_how_many_rows_a_token_has(monkeypatch):
     assert quantize(monkeypatch, inv.reshape(2, 2, 2), None) == B.MOE_ERR_SHAPE
     assert quantize(monkeypatch, inv[:6].reshape(3, 2), None) == B.MOE_ERR_SHAPE
     assert quantize(monkeypatch, inv.reshape(2, 4), None, T=1) == B.MOE_ERR_SHAPE     # two tokens, one row of them
+
+
+def test_tiles_are_not_selected_without_a_handle():
+    with pytest.raises(B.MoeError) as e:
+        B.moe_mxfp4_select_tile(None, 4, 2, 16)
+    assert e.value.code == B.MOE_ERR_NULL
