@@ -278,6 +278,7 @@ constexpr int kPrWScaleBytes = 2 * kMxTileBytes, kPrXScaleBytes = 4 * kMxTileByt
 constexpr int kPrScaleCols = 24;                            // TMEM columns of a stage's exponents: weights 2 x 4, rows 2 x 8
 constexpr int kPrTmemCols = 512;
 constexpr int kPrMaxStages = 8;
+constexpr unsigned long long kPrLandNs = 1000000ull;       // 1 ms: a whole device has 31 MB on their way, 5 us at the measured copy bandwidth
 constexpr int kMaxExperts = 1024;
 // results on their way out: 32 rows x 64 columns, two of them for every two epilogue warps
 constexpr int kPrOutRows = 32, kPrOutCols = 64, kPrOutBytes = kPrOutRows * kPrOutCols * 2, kPrOutUnits = kPrEpiWarps / 2;
@@ -492,7 +493,7 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
     constexpr uint32_t kAt = kWhat == kLoadW ? 0 : kWhat == kLoadX ? kPrWBytes : kWhat == kLoadWs ? kPrWBytes + C::kXBytes : kPrWBytes + C::kXBytes + kPrWScaleBytes;
     constexpr int kStep = kWhat == kLoadW || kWhat == kLoadX ? kPrK / 2 : 2;
     const uint32_t dst0 = smem_u32(ring) + kAt, empty0 = smem_u32(&ctl->empty[0]), full0 = smem_u32(&ctl->full[0]);
-    uint32_t dst = dst0, empty_bar = empty0, full_bar = full0, phase = 0, armed = 0;
+    uint32_t dst = dst0, empty_bar = empty0, full_bar = full0, phase = 0;
     bool ok = true, ready = true;                              // (all stages are free at first)
     for (; walk.g < total && ok; walk.next()) {
         const ProductTile t = walk.tile(P, ctl);
@@ -544,7 +545,6 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
                     else tma_load_3d(dst, map, bar, 0, x, y);
                 }
             }
-            armed = min(armed + 1u, (uint32_t)C::kStages);
             x += kStep;
             dst += (uint32_t)C::kStageBytes;
             empty_bar += 8u;
@@ -556,15 +556,6 @@ __device__ __forceinline__ void product_loader(const ProductParams &P, ProductCo
                 phase ^= 1u;
             }
             ready = mbar_test_wait(empty_bar, phase ^ 1u);
-        }
-    }
-    if ((!ok || ctl->abort) && rank == 0) {
-        // wind-down: the copies already issued land before shared memory is released
-        const int stage = (int)(empty_bar - empty0) >> 3;
-        const unsigned long long drain = globaltimer_ns() + 2000000ull;
-        for (int i = 0; i < C::kStages; ++i) {
-            if (i >= stage && armed < (uint32_t)C::kStages) continue;
-            while (!mbar_try_wait(smem_u32(&ctl->full[i]), i < stage ? phase : phase ^ 1u) && globaltimer_ns() < drain) {}
         }
     }
     __syncwarp();
@@ -765,16 +756,6 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
             }
             advance();
         }
-        if (!ok) {
-            // what was issued finishes before shared memory and TMEM are released
-            if (elect_one_sync()) {
-                if (kPair) tc_commit_pair(smem_u32(&ctl->drain));
-                else tc_commit(smem_u32(&ctl->drain));
-            }
-            __syncwarp();
-            const unsigned long long until = globaltimer_ns() + 2000000ull;
-            while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < until) {}
-        }
         __syncwarp();
     } else if (warp >= 4 && warp < 4 + kPrEpiWarps) {
         const int q4 = warp & 3, grp = (warp - 4) >> 2;
@@ -833,9 +814,24 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         }
         if (kPair && (q4 & 1) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
-    // (pair: nobody leaves while the other CTA may still touch its memory)
     tc_fence_before();
     __syncthreads();
+    // After a wait that ran out, roles have left without waiting for one another: the MMAs that were issued finish, and the copies that are on
+    // their way land, before TMEM and shared memory are given back.  (A pair's copies complete on the first CTA's barriers, so that the second
+    // has none to wait on: every CTA waits for a time that copies do not take.)
+    if (ctl->abort) {
+        const unsigned long long now = globaltimer_ns();
+        if (warp == 1 && rank == 0) {
+            if (elect_one_sync()) {
+                if (kPair) tc_commit_pair(smem_u32(&ctl->drain));
+                else tc_commit(smem_u32(&ctl->drain));
+            }
+            __syncwarp();
+            while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < now + 4 * kPrLandNs) {}
+        }
+        while (globaltimer_ns() < now + kPrLandNs) {}
+    }
+    // (pair: nobody leaves while the other CTA may still touch its memory)
     if (kPair) cluster_sync_all();
     if (warp == 1) {
         tc_fence_after();

@@ -125,3 +125,36 @@ def test_all_families_on_streams_of_their_own():
     for offsets, _, _, _, _, xv, wv, _, out, st, _ in jobs:
         check_wide(out[0], xv, wv, offsets, xv.shape[1])
         assert torch.equal(*out) and st.tolist() == [0, 0, 0, 0]
+
+
+# ----------------------------------------------------------------------------- waits that run out
+
+# Sizes whose tiles take several times the 64 polls (90 us) after which a wait looks at its limit, three and more tiles for a CTA or pair: the results'
+# warps give up in the first, the issuer and the loaders where those no longer hand accumulators and stages back.
+LONG = [(16, 444 * 128, 1 << 17, FEW), (4100, 21 * 128, 1 << 18, ONE), (5400, 29 * 256, 1 << 18, PAIR)]
+VALUES = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+
+
+@pytest.mark.parametrize("rows, N, K, tile", LONG)
+def test_a_wait_that_runs_out_is_reported_and_the_context_survives(rows, N, K, tile):
+    assert select(rows, 1, N) == tile
+    # row r of x is one value all along, column n of the weights another: every partial sum is 1, 3 or 9 times a power of two times up to 2^18, exact in fp32
+    code = lambda n: (torch.arange(n, device="cuda") % 8 * 17).to(torch.uint8).reshape(-1, 1).expand(n, K // 2).contiguous()  # noqa: E731
+    scales = lambda n: torch.full((B.moe_mxfp4_scale_bytes(n, K, 1),), 127, dtype=torch.uint8, device="cuda")  # noqa: E731
+    xc, wc, xs, ws, off = code(rows), code(N).reshape(1, N, K // 2), scales(rows), scales(N), ints([0, rows])
+    out, st = torch.full((rows, N), 7.0, dtype=torch.bfloat16, device="cuda"), status()
+    B.moe_set_wait_limit_ns(handle(), 1000)
+    try:
+        B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, off, out, st)
+        torch.cuda.synchronize()
+    finally:
+        B.moe_set_wait_limit_ns(handle(), 2_000_000_000)
+    assert B.moe_get_status(handle(), st, check=False).code == B.MOE_DEV_TIMEOUT
+    v = torch.tensor(VALUES, device="cuda")
+    want = v[torch.arange(rows, device="cuda") % 8].reshape(-1, 1) * v[torch.arange(N, device="cuda") % 8] * K
+    # what was written before the limit is right, and not all of it was
+    assert ((out == 7.0) | (out == want)).all() and (out == 7.0).any()
+    for _ in range(2):
+        st = status()
+        B.moe_mxfp4_gemm(handle(), xc, xs, wc, ws, off, out, st)
+        assert st.tolist() == [0, 0, 0, 0] and (out == want).all()
