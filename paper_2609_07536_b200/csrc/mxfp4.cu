@@ -39,7 +39,7 @@ struct Quant {
     int32_t rows, src_rows, copies, groups, n_even;
     int32_t K, KQ, lanes, rows_per_cta;   // KQ = ceil(K / 128); lanes: threads of a row, 8 per 128 columns
     int32_t wide;                  // 16 columns of the 16- or 32-bit matrix are on 32-byte boundaries
-    Divisor by_lanes, by_copies, by_n;
+    Divisor by_lanes, by_n;
 };
 struct QuantRow {
     uint8_t *codes, *scales;       // the row's codes (nullptr: it has no place), its first exponent byte

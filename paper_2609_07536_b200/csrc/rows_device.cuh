@@ -23,12 +23,6 @@ __device__ __forceinline__ uint2 ld_row_v2(const void *p)
     asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t ld_row_u32(const void *p)
-{
-    uint32_t v;
-    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
 __device__ __forceinline__ uint32_t ld_row_u8(const void *p)
 {
     uint32_t v;
