@@ -850,12 +850,14 @@ static_assert(pr_smem_bytes<kOneTiles>() <= 227 * 1024 && pr_smem_bytes<kPairTil
 //   N 2048, K 1408  100 (10) 26.3/26.9   136 (11) 29.8/29.8   157 (13) 35.3/33.9   181 (14) 36.1/35.0   248 (16) 42.9/40.9   992 (44) 132/113
 //   N 1536, K 512   200 (6) 14.4/15.0    300 (8) 17.5/18.6    409 (10) 20.6/21.5   520 (12) 22.7/23.4   819 (17) 30.8/30.8   1638 (31) 52.0/49.5
 //   N 1024, K 1536  200 (4) 17.5/18.5    300 (6) 20.5/20.7    409 (7) 23.2/22.8    819 (11) 35.7/34.0   1638 (20) 62.7/56.5
+// Within 2 % of the line either side may be ahead: the rule loses 3 % at N 1536, K 512 with 12 tiles, whose short K hides a pair's start least.
 constexpr int32_t kPairRowsPerExpert = 128, kPairTilesEach = 11;
-// Mean rows per expert up to which tiles of 64 rows in eight stages pay: 168 KB on their way to an SM instead of 105, but an expert of 65 rows reads its
-// weights twice.  192 / 64 rows, us, at 1 / 4 to 6 / 7 to 8 / 15 to 17 / 48 rows per expert:
+// Mean rows per expert up to which tiles of 64 rows in eight stages pay: with up to 16 rows in a tile 160 KB are on their way to an SM instead of 105
+// (with 64 rows 208 instead of 135), but an expert of 65 rows reads its weights twice.  192 / 64 rows, us, at 1 / 4 to 6 / 7 to 8 / 15 to 17 / 48 rows per expert:
 //   N 2816, K 2048   22.8/21.9  34.2/33.8  35.9/36.4  36.9/37.6  40.5/42.2
 //   N 2048, K 1408   16.4/15.4  20.8/19.2  22.5/21.0  23.8/22.2  25.8/24.7
 //   N 1024, K 1536    9.4/9.3   11.3/10.9  12.0/11.6  12.2/11.9  12.7/12.3
+// The rule goes by rows alone, and loses 1 to 2 % where the weights are largest (N 2816, K 2048 from seven rows on), as it leaves 4 % at 48 rows elsewhere.
 constexpr int32_t kFewRowsPerExpert = 16;
 
 // tiles of a launch, whatever the offsets
