@@ -610,6 +610,25 @@ __device__ __noinline__ void count_tiles(const ProductParams &P, ProductControl 
     }
 }
 
+// After a wait that ran out, roles have left without waiting for one another: the MMAs that were issued finish, and the copies that are on
+// their way land, before TMEM and shared memory are given back.  By the warp that issues the MMAs, in each CTA of a pair: a pair's copies
+// complete on the first CTA's barriers, so that the second has none to wait on, and every CTA waits for a time that copies do not take.
+template <bool kPair>
+__device__ __noinline__ void finish_in_flight(ProductControl *ctl, uint32_t rank)
+{
+    const unsigned long long now = globaltimer_ns();
+    if (rank == 0) {
+        if (elect_one_sync()) {
+            if (kPair) tc_commit_pair(smem_u32(&ctl->drain));
+            else tc_commit(smem_u32(&ctl->drain));
+        }
+        __syncwarp();
+        while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < now + 4 * kPrLandNs) {}
+    }
+    while (globaltimer_ns() < now + kPrLandNs) {}
+    __syncwarp();
+}
+
 template <class E, int kKind>
 __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __grid_constant__ ProductParams P)
 {
@@ -648,8 +667,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     if (P.E <= kPrThreads - 1) {
         const int e = (int)threadIdx.x;
         const int o = ld_chained(P.offsets + min(e, P.E)), next = ld_chained(P.offsets + min(e + 1, P.E));
-        const bool ordered = o >= 0 && o <= next && next <= P.R;
-        int t = e < P.E && ordered ? (next - o + C::kRows - 1) / C::kRows : 0;
+        int t = e < P.E ? (int)(((uint32_t)next - (uint32_t)o + (uint32_t)(C::kRows - 1)) / (uint32_t)C::kRows) : 0;      // (in order: as below)
         const int own = t;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -659,7 +677,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
         if (e <= P.E) ctl->first[e] = o;
         if (lane == 31) ctl->warp_tiles[warp] = t;
         tc_fence_before();
-        const bool fine = __syncthreads_and(ordered) != 0;
+        const bool fine = __syncthreads_and(o >= 0 && o <= next && next <= P.R) != 0;
         tc_fence_after();
         if (fine && 32 * warp <= P.E) {
             int base = 0;
@@ -816,21 +834,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) mxfp4_product_kernel(const __gr
     }
     tc_fence_before();
     __syncthreads();
-    // After a wait that ran out, roles have left without waiting for one another: the MMAs that were issued finish, and the copies that are on
-    // their way land, before TMEM and shared memory are given back.  (A pair's copies complete on the first CTA's barriers, so that the second
-    // has none to wait on: every CTA waits for a time that copies do not take.)
-    if (ctl->abort) {
-        const unsigned long long now = globaltimer_ns();
-        if (warp == 1 && rank == 0) {
-            if (elect_one_sync()) {
-                if (kPair) tc_commit_pair(smem_u32(&ctl->drain));
-                else tc_commit(smem_u32(&ctl->drain));
-            }
-            __syncwarp();
-            while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < now + 4 * kPrLandNs) {}
-        }
-        while (globaltimer_ns() < now + kPrLandNs) {}
-    }
+    if (warp == 1 && ctl->abort) finish_in_flight<kPair>(ctl, rank);
     // (pair: nobody leaves while the other CTA may still touch its memory)
     if (kPair) cluster_sync_all();
     if (warp == 1) {
