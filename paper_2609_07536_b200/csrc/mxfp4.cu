@@ -51,7 +51,8 @@ __device__ __forceinline__ void hold_offsets(const Quant &p, int32_t *held)
     if (p.offsets && p.groups <= kQuantGroupsHeld)
         for (int g = threadIdx.x; g <= p.groups; g += kQuantThreads) held[g] = ld_chained(p.offsets + g);
 }
-__device__ __forceinline__ bool ordered(const Quant &p, int begin, int end) { return begin >= 0 && begin <= end && end <= p.rows; }
+// 0 <= begin <= end <= rows
+__device__ __forceinline__ bool ordered(const Quant &p, int begin, int end) { return (uint32_t)begin <= (uint32_t)end && (uint32_t)end <= (uint32_t)p.rows; }
 // All threads meet here; false: offsets that are not in order, or more than are held.  The last threads look them over, while the first
 // ones find their rows.
 __device__ __forceinline__ bool meet_with_offsets_ordered(const Quant &p, const int32_t *held)
