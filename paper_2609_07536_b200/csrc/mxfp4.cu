@@ -585,7 +585,7 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
 // the rows, and where it begins behind the rows of all such experts before it; tiles of any other are never walked to.
 __device__ __noinline__ void count_tiles(const ProductParams &P, ProductControl *ctl, int lane, int tile_rows)
 {
-    int tiles = 0, top = 0;                      // of the experts before this round of 32: their tiles, where their rows end
+    int tiles = 0, top = 0;                      // of the experts before these 32: their tiles, where their rows end
     for (int e0 = 0; e0 <= P.E; e0 += 32) {
         const int e = e0 + lane, begin = ctl->first[min(e, P.E)], end = ctl->first[min(e + 1, P.E)];
         const bool ordered = begin >= 0 && begin <= end && end <= P.R;

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kRowThreads) spread_kernel(const __grid_consta
 // kAhead loads in flight a thread.  The blocks stay: a warp looks up the indexes of its next piece while the rows of this one are on their
 // way, so that the one latency does not lie in front of the other in every piece (16384 tokens, 8 rows each of 4 KB: 95 us, 98 % of the
 // measured copy bandwidth; a block for every eight pieces 107).  Eight loads from five rows a token on: four leave more blocks to an SM, but
-// have a second round then.  Four / eight, us, 16384 tokens of 4 KB, 1 / 2 / 4 / 5 / 6 / 8 / 12 rows each: 33.1/47.4  40.1/51.4  54.9/62.2  70.6/69.0
+// then take two turns.  Four / eight, us, 16384 tokens of 4 KB, 1 / 2 / 4 / 5 / 6 / 8 / 12 rows each: 33.1/47.4  40.1/51.4  54.9/62.2  70.6/69.0
 // 78.6/77.1  95.8/95.4  137.2/140.0; 1003 tokens of 3 KB, 4 / 5 / 6 / 8 rows: 4.1/4.1  4.1/4.6  4.8/4.8  6.2/5.5 (five rows of few tokens and twelve
 // of many lose 0.5 and 3 us by the rule).
 template <class E, bool kWeighted, int kAhead>
