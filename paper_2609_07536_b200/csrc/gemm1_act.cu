@@ -492,6 +492,7 @@ moe_gemm1_act_kernel(const __grid_constant__ G1Params P)
     // ---------------- teardown (pair: nobody leaves while its peer may still touch its memory)
     tc_fence_before();
     __syncthreads();
+    if (warp == 1 && ctl->abort) wait_for_what_is_in_flight();
     if (kPair) cluster_sync_all();
     if (warp == 1) {
         tc_fence_after();

@@ -777,6 +777,7 @@ __device__ void compute_cta(const FusedParams &P, const Part &pt, uint8_t *ring,
     tc_fence_before();
     sync_compute_warps(P);
     if (warp == 1) {
+        if (ctl->abort) wait_for_what_is_in_flight();
         tc_fence_after();
         tmem_dealloc(tmem_base, C::kTmemCols);
     }
@@ -941,6 +942,7 @@ __device__ __forceinline__ void compute_cta_pair(const FusedParams &P, const Par
     // communication warps arrived on this cluster barrier at once)
     tc_fence_before();
     sync_compute_warps(P);
+    if (warp == 1 && ctl->abort) wait_for_what_is_in_flight();
     cluster_sync_all();
     if (warp == 1) {
         tc_fence_after();

@@ -279,7 +279,6 @@ constexpr int kPrWScaleBytes = 2 * kMxTileBytes, kPrXScaleBytes = 4 * kMxTileByt
 constexpr int kPrScaleCols = 24;                            // TMEM columns of a stage's exponents: weights 2 x 4, rows 2 x 8
 constexpr int kPrTmemCols = 512;
 constexpr int kPrMaxStages = 8;
-constexpr unsigned long long kPrLandNs = 1000000ull;       // 1 ms: a whole device has 31 MB on their way, 5 us at the measured copy bandwidth
 constexpr int kMaxExperts = 1024;
 // results on their way out: 32 rows x 64 columns, two of them for every two epilogue warps
 constexpr int kPrOutRows = 32, kPrOutCols = 64, kPrOutBytes = kPrOutRows * kPrOutCols * 2, kPrOutUnits = kPrEpiWarps / 2;
@@ -624,10 +623,9 @@ __device__ __noinline__ void finish_in_flight(ProductControl *ctl, uint32_t rank
             else tc_commit(smem_u32(&ctl->drain));
         }
         __syncwarp();
-        while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < now + 4 * kPrLandNs) {}
+        while (!mbar_try_wait(smem_u32(&ctl->drain), 0u) && globaltimer_ns() < now + 4 * kLandNs) {}
     }
-    while (globaltimer_ns() < now + kPrLandNs) {}
-    __syncwarp();
+    wait_for_what_is_in_flight();
 }
 
 template <class E, int kKind>

@@ -386,6 +386,16 @@ __device__ __forceinline__ void tmem_ld_16x256_x4(uint32_t taddr, uint32_t (&r)[
         : "r"(taddr)
         : "memory");
 }
+// After a wait that ran out, by one warp of the CTA, before TMEM and shared memory are given back: roles have left without waiting for one
+// another, so MMAs that were issued and copies of operands may still be on their way.  1 ms: a whole device has 31 MB of operands on their way,
+// 5 us at the measured copy bandwidth, and a ring of them is as many MMAs.
+constexpr unsigned long long kLandNs = 1000000ull;
+__device__ __forceinline__ void wait_for_what_is_in_flight()
+{
+    const unsigned long long now = globaltimer_ns();
+    while (globaltimer_ns() < now + kLandNs) {}
+    __syncwarp();
+}
 // two fp32 -> bf16, the first one in the lower half
 __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi)
 {
